@@ -1,5 +1,5 @@
 """Python binding of libtschain.so: marshals torch tensors (device memory and the
-current HIP stream) into the C ABI of include/ts_chain.h.  No arithmetic happens here;
+current HIP stream) into the C ABI of include/ts_chain.h and include/ts_token.h.  No arithmetic happens here;
 every step runs in the library's HIP kernels.  If the library is missing, every call
 raises: there is no fallback."""
 import ctypes
@@ -12,8 +12,11 @@ LIB_PATH = os.path.join(HERE, "libtschain.so")
 
 OP_LOGPARTITION, OP_MARGINALS, OP_VITERBI, OP_MARGINALS_VITERBI = 0, 1, 2, 3
 OP_ENTROPY, OP_LOG_DENSITY, OP_SAMPLE = 4, 5, 6
+TOKEN_TOP, TOKEN_DISTILL, TOKEN_DISTILL_GRAD, TOKEN_VERIFY = 0, 1, 2, 3
 STATUS = {0: "TS_OK", -1: "TS_ERR_NULL_ARG", -2: "TS_ERR_BAD_DIM", -3: "TS_ERR_WORKSPACE",
-          -4: "TS_ERR_LENGTHS", -5: "TS_ERR_HIP", -6: "TS_ERR_LABELS"}
+          -4: "TS_ERR_LENGTHS", -5: "TS_ERR_HIP", -6: "TS_ERR_LABELS",
+          -7: "TS_ERR_BAD_ARG"}
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 _lib = None
 
@@ -50,7 +53,20 @@ def lib():
         L.ts_semimarkov_logpartition.argtypes = [p, p, i64, i64, i64, i64, p, p, sz, p]
         L.ts_semimarkov_marginals.argtypes = [p, p, i64, i64, i64, i64, p, p, p, sz, p]
         L.ts_semimarkov_viterbi.argtypes = [p, p, i64, i64, i64, i64, p, p, p, p, sz, p]
-        for f in ("ts_chain_logpartition", "ts_chain_marginals", "ts_chain_viterbi",
+        f32, ci = ctypes.c_float, ctypes.c_int
+        L.ts_token_max_vocab.restype = ci
+        L.ts_token_max_top.restype = ci
+        L.ts_token_workspace_bytes.argtypes = [ci, i64, i64, i64, i64]
+        L.ts_token_workspace_bytes.restype = sz
+        L.ts_token_top.argtypes = [p, ci, i64, i64, p, i64, i64, i64, i64, f32, p, p, p, p, sz, p]
+        L.ts_token_distill.argtypes = [p, ci, i64, i64, p, ci, p, p, p, i64, i64, i64, i64, f32, p,
+                                       p, sz, p]
+        L.ts_token_distill_grad.argtypes = [p, ci, i64, i64, p, ci, p, p, p, p, i64, i64, i64, i64,
+                                            f32, p, p, p, sz, p]
+        L.ts_token_verify.argtypes = [p, ci, i64, i64, p, ci, i64, i64, p, p, p, p, p, i64, i64,
+                                      i64, f32, f32, p, p, p, p, sz, p]
+        for f in ("ts_token_top", "ts_token_distill", "ts_token_distill_grad", "ts_token_verify",
+                  "ts_chain_logpartition", "ts_chain_marginals", "ts_chain_viterbi",
                   "ts_chain_marginals_noalloc",
                   "ts_chain_marginals_viterbi", "ts_chain_entropy", "ts_chain_log_density",
                   "ts_chain_logpartition_sequential", "ts_chain_sample",
@@ -300,3 +316,150 @@ def semi_viterbi(sp, lengths=None, out=None, ws=None):
                                        _ptr(seglen) if N > 1 else None, _ptr(score), _ptr(w),
                                        nb, _stream(sp.device)))
     return path, seglen, score
+
+
+# ---- rows of token logits [B, N, V] (include/ts_token.h) ----
+
+def _prep_rows(x, name):
+    """x with its rows contiguous (copied only where they are not), its type's code and the
+    elements from a sequence, a row to the next."""
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if x.dtype not in DTYPES or x.dim() != 3:
+        raise ValueError(f"{name} must be float32, bfloat16 or float16 [B, N, V]")
+    if x.shape[2] > 1 and x.stride(2) != 1:
+        x = x.contiguous()
+    return x, DTYPES[x.dtype], x.stride(0), x.stride(1)
+
+
+def _prep_small(x, name, dtype, shape, device):
+    if x is None:
+        return None
+    if x.dtype != dtype or x.shape != shape or x.device != device:
+        raise ValueError(f"{name} must be {dtype} {list(shape)} on the same device as the logits")
+    return x if x.is_contiguous() else x.contiguous()
+
+
+def _prep_out(x, name, dtype, shape, device):
+    x = _prep_small(x, name, dtype, shape, device)
+    return torch.empty(shape, dtype=dtype, device=device) if x is None else x
+
+
+def _prep_outs(out, names, dtypes, shapes, device):
+    for x, name in zip(out or (), names):
+        if x is not None and not x.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    out = out or (None,) * len(names)
+    if len(out) != len(names):
+        raise ValueError(f"out must be ({', '.join(names)})")
+    return [_prep_out(*a, device) for a in zip(out, names, dtypes, shapes)]
+
+
+def token_workspace_bytes(op, B, N, V, K=1):
+    return lib().ts_token_workspace_bytes(op, B, N, V, K)
+
+
+def _token_workspace(op, B, N, V, K, device, ws):
+    if ws is not None:
+        return ws, ws.numel() * ws.element_size()
+    need = token_workspace_bytes(op, B, N, V, K)
+    if need == 0:
+        return None, 0
+    return torch.empty(need, dtype=torch.uint8, device=device), need
+
+
+def top_logits(logits, K, lengths=None, temperature=1.0, out=None, ws=None):
+    """(values [B, N, K] of the logits' type, indices int32 [B, N, K], lse float32 [B, N]): the K
+    largest logits of every row of logits [B, N, V], largest first and equal ones by the lowest
+    index, and log sum exp(logits / temperature).  Rows from lengths (int32 [B]) on are padding:
+    values and lse -inf, indices -1."""
+    logits, dtype, sb, sn = _prep_rows(logits, "logits")
+    B, N, V = logits.shape
+    dev = logits.device
+    lengths = _prep_small(lengths, "lengths", torch.int32, (B,), dev)
+    values, indices, lse = _prep_outs(
+        out, ("values", "indices", "lse"), (logits.dtype, torch.int32, torch.float32),
+        ((B, N, K), (B, N, K), (B, N)), dev)
+    w, nb = _token_workspace(TOKEN_TOP, B, N, V, K, dev, ws)
+    _check(lib().ts_token_top(_ptr(logits), dtype, sb, sn, _ptr(lengths), B, N, V, K, temperature,
+                              _ptr(values), _ptr(indices), _ptr(lse), _ptr(w), nb, _stream(dev)))
+    return values, indices, lse
+
+
+def _prep_teacher(logits, top_values, top_indices, top_lse, lengths):
+    logits, dtype, sb, sn = _prep_rows(logits, "logits")
+    B, N, V = logits.shape
+    dev = logits.device
+    if top_values.dtype not in DTYPES or top_values.dim() != 3:
+        raise ValueError("top_values must be float32, bfloat16 or float16 [B, N, K]")
+    K = top_values.shape[2]
+    top_values = _prep_small(top_values, "top_values", top_values.dtype, (B, N, K), dev)
+    top_indices = _prep_small(top_indices, "top_indices", torch.int32, (B, N, K), dev)
+    top_lse = _prep_small(top_lse, "top_lse", torch.float32, (B, N), dev)
+    lengths = _prep_small(lengths, "lengths", torch.int32, (B,), dev)
+    head = (_ptr(logits), dtype, sb, sn, _ptr(top_values), DTYPES[top_values.dtype],
+            _ptr(top_indices), _ptr(top_lse))
+    # the tensors themselves are returned too: copies made here have to outlive the launch
+    return head, (logits, top_values, top_indices, top_lse, lengths), (B, N, V, K), dev
+
+
+def distill(logits, top_values, top_indices, top_lse=None, lengths=None, temperature=1.0, out=None,
+            ws=None):
+    """Kullback-Leibler divergence [B, N] (float32) of softmax(logits / temperature), logits
+    [B, N, V], from a teacher's top logits: values [B, N, K] at indices int32 [B, N, K] (an index
+    outside the vocabulary is an empty slot).  Without top_lse the teacher is normalised over
+    its slots; with it (its log-sum-exp [B, N] at this temperature) what they leave is one class.
+    0 for padding."""
+    head, kept, (B, N, V, K), dev = _prep_teacher(logits, top_values, top_indices, top_lse, lengths)
+    loss, = _prep_outs(None if out is None else (out,), ("loss",), (torch.float32,), ((B, N),), dev)
+    w, nb = _token_workspace(TOKEN_DISTILL, B, N, V, K, dev, ws)
+    _check(lib().ts_token_distill(*head, _ptr(kept[-1]), B, N, V, K, temperature, _ptr(loss),
+                                  _ptr(w), nb, _stream(dev)))
+    return loss
+
+
+def distill_grad(logits, top_values, top_indices, top_lse=None, lengths=None, weights=None,
+                 temperature=1.0, out=None, ws=None, want_loss=True):
+    """(loss [B, N] or None as distill()'s, grad [B, N, V] of the logits' type): the gradient of
+    sum(weights * loss) by the logits, weights float32 [B, N] (None: all 1)."""
+    head, kept, (B, N, V, K), dev = _prep_teacher(logits, top_values, top_indices, top_lse, lengths)
+    weights = _prep_small(weights, "weights", torch.float32, (B, N), dev)
+    loss, grad = _prep_outs(out, ("loss", "grad"), (torch.float32, logits.dtype),
+                            ((B, N), (B, N, V)), dev)
+    w, nb = _token_workspace(TOKEN_DISTILL_GRAD, B, N, V, K, dev, ws)
+    _check(lib().ts_token_distill_grad(*head, _ptr(weights), _ptr(kept[-1]), B, N, V, K,
+                                       temperature, _ptr(loss) if want_loss else None, _ptr(grad),
+                                       _ptr(w), nb, _stream(dev)))
+    return (loss if want_loss else None), grad
+
+
+def verify(target, draft, tokens, uniforms, noise, lengths=None, draft_lse=None, temperature=1.0,
+           draft_temperature=1.0, out=None, ws=None):
+    """(out int32 [B, G+1], accepted int32 [B], logp float32 [B, G+1]): the drafts tokens (int32
+    [B, G]) that the target's probabilities accept, then one more token, then -1; the number of
+    accepted ones; the target's log-probabilities of what is emitted.  target [B, G+1, V] and
+    draft [B, G, V] are logits, draft_lse [B, G] the drafts' log-sum-exps where they are known
+    (0 for log-probabilities), uniforms float32 [B, G] in [0, 1) and noise float32 [B, V]
+    (standard exponentials) the caller's random numbers, lengths (int32 [B]) the drafts of each
+    sequence."""
+    target, dtype, sb, sn = _prep_rows(target, "target")
+    B, G, V = target.shape[0], target.shape[1] - 1, target.shape[2]
+    dev = target.device
+    draft, ddtype, db, dn = _prep_rows(draft, "draft")
+    if draft.shape != (B, G, V) or draft.device != dev:
+        raise ValueError(f"draft must be {[B, G, V]} on the same device as the target")
+    tokens = _prep_small(tokens, "tokens", torch.int32, (B, G), dev)
+    uniforms = _prep_small(uniforms, "uniforms", torch.float32, (B, G), dev)
+    noise = _prep_small(noise, "noise", torch.float32, (B, V), dev)
+    draft_lse = _prep_small(draft_lse, "draft_lse", torch.float32, (B, G), dev)
+    lengths = _prep_small(lengths, "lengths", torch.int32, (B,), dev)
+    emitted, accepted, logp = _prep_outs(
+        out, ("out", "accepted", "logp"), (torch.int32, torch.int32, torch.float32),
+        ((B, G + 1), (B,), (B, G + 1)), dev)
+    w, nb = _token_workspace(TOKEN_VERIFY, B, G, V, 1, dev, ws)
+    _check(lib().ts_token_verify(_ptr(target), dtype, sb, sn, _ptr(draft), ddtype, db, dn,
+                                 _ptr(draft_lse), _ptr(tokens), _ptr(uniforms), _ptr(noise),
+                                 _ptr(lengths), B, G, V, temperature, draft_temperature,
+                                 _ptr(emitted), _ptr(accepted), _ptr(logp), _ptr(w), nb,
+                                 _stream(dev)))
+    return emitted, accepted, logp
