@@ -4,10 +4,11 @@
 // argmax_v r_v / e_v, r = max(p_a - q_a, 0) where draft a was refused and p_a otherwise, e_v the
 // given exponentials: v's clock, of rate r_v, rings first with probability r_v / sum r.
 //
-// Two launches: the softmax statistics of every row in parts, one workgroup each; then, for
-// every sequence, the tests (a few numbers, which each of its workgroups does by itself) and
-// the race over the one row that the next token is drawn from, in parts whose winners meet in
-// a maximum over (score, ~index) words, which no order of arrival changes.
+// k_verify_stats sums rows in parts, one workgroup each (maximum and sum of the softmax).
+// k_verify_draw runs the race over the one row of every sequence that its next token is drawn
+// from, again in parts, whose winners meet in a maximum over (score, ~index) words, which no
+// order of arrival changes.  Which row that is, each workgroup finds out by itself: the tests
+// are a few numbers a draft.
 #include <hip/hip_runtime.h>
 
 #include "token.h"
@@ -15,11 +16,18 @@
 namespace tsc {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kPartElems = 16384;   // elements of a row that one workgroup sums
+constexpr int kStatThreads = 256;
+constexpr int kDrawThreads = 512;
+constexpr int kMaxParts = kWave;   // parts of a row: one a lane when they are joined
+constexpr int kMinPart = 2048;     // elements of a part: 8 a thread
 
-__host__ __device__ inline int parts_of(int64_t V) {
-    return (int)((V + kPartElems - 1) / kPartElems);
+// Parts of a row: enough workgroups to fill the chip where the rows are few
+inline int parts_of(int64_t rows, int64_t V, int64_t want) {
+    int64_t p = (want + rows - 1) / rows;
+    const int64_t most = (V + kMinPart - 1) / kMinPart;
+    if (p > most) p = most;
+    if (p > kMaxParts) p = kMaxParts;
+    return p < 1 ? 1 : (int)p;
 }
 __device__ __forceinline__ void part_range(int V, int parts, int part, int* lo, int* hi) {
     // multiples of 64 elements, so that parts of an aligned row are aligned
@@ -29,31 +37,40 @@ __device__ __forceinline__ void part_range(int V, int parts, int part, int* lo, 
 }
 
 struct Plan {
-    int parts;
+    int parts, draw_parts;
     float2* stats;    // [B][2][G + 1][parts]: target's, draft's maximum and sum
+    float* logit;     // [B][2][G + 1]: their logits of the draft
     uint64_t* best;   // [B] the race's largest word so far
     int32_t* left;    // [B] parts of the race that have not arrived
     size_t bytes;
 };
 inline Plan plan_of(int64_t B, int64_t G, int64_t V, void* ws) {
     Plan p;
-    p.parts = parts_of(V);
+    p.parts = parts_of(B * (2 * G + 1), V, 4096);
+    p.draw_parts = parts_of(B, V, 1024);
     char* base = (char*)ws;
-    const size_t n = (size_t)B * 2 * (G + 1) * p.parts;
-    p.stats = (float2*)base;
-    size_t off = (n * sizeof(float2) + 255) / 256 * 256;
-    p.best = (uint64_t*)(base + off);
-    off += ((size_t)B * sizeof(uint64_t) + 255) / 256 * 256;
-    p.left = (int32_t*)(base + off);
-    off += ((size_t)B * sizeof(int32_t) + 255) / 256 * 256;
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        char* at = base + off;
+        off += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    const size_t rows = (size_t)B * 2 * (G + 1);
+    p.stats = (float2*)take(rows * p.parts * sizeof(float2));
+    p.logit = (float*)take(rows * sizeof(float));
+    p.best = (uint64_t*)take((size_t)B * sizeof(uint64_t));
+    p.left = (int32_t*)take((size_t)B * sizeof(int32_t));
     p.bytes = off;
     return p;
 }
+__device__ __forceinline__ int64_t row_index(const VerifyArgs& a, int64_t b, int side, int64_t t) {
+    return (b * 2 + side) * (a.G + 1) + t;
+}
 
-// One workgroup per (side, position, part, sequence): maximum and sum of a part of a row
+// One workgroup per (sequence, side and position, part): maximum and sum of a part of a row
 template <class TT, class TD>
-__global__ __launch_bounds__(kThreads) void k_verify_stats(VerifyArgs a, Plan p) {
-    __shared__ float2 red[kThreads / kWave];
+__global__ __launch_bounds__(kStatThreads) void k_verify_stats(VerifyArgs a, Plan p) {
+    __shared__ float2 red[kStatThreads / kWave];
     const int64_t per = (int64_t)p.parts * (2 * a.G + 1);
     for (int64_t i = blockIdx.x; i < per * a.B; i += gridDim.x) {
         const int64_t b = i / per;
@@ -61,34 +78,34 @@ __global__ __launch_bounds__(kThreads) void k_verify_stats(VerifyArgs a, Plan p)
         const int64_t r = i % per / p.parts;
         const bool drafted = r > a.G;
         const int64_t t = drafted ? r - a.G - 1 : r;
+        const int64_t n = clamp_rows(a.lengths, b, a.G);
         if (r == 0 && part == 0 && threadIdx.x == 0) {
             p.best[b] = 0;
-            p.left[b] = p.parts;
+            p.left[b] = p.draw_parts;
         }
-        if (t >= clamp_rows(a.lengths, b, a.G) + (drafted ? 0 : 1) || (drafted && a.draft_lse))
-            continue;
+        if (t >= n + (drafted ? 0 : 1)) continue;
+        const TT* x = row_of<TT>(a.target, b, t);
+        const TD* y = drafted ? row_of<TD>(a.draft, b, t) : nullptr;
+        const int64_t row = row_index(a, b, drafted, t);
+        if (part == 0 && threadIdx.x == 0 && t < n) {
+            const int z = a.tokens[b * a.G + t];
+            // (what is no token is refused: the target gives it nothing)
+            p.logit[row] = z < 0 || z >= a.V ? -INFINITY : drafted ? to_f(y[z]) : to_f(x[z]);
+        }
+        if (drafted && a.draft_lse) continue;
         int lo, hi;
         part_range(a.V, p.parts, part, &lo, &hi);
         Soft s = soft_empty();
         const float c = drafted ? a.draft_scale.c : a.scale.c;
         if (drafted)
-            walk_row<TD, kThreads, 4>(row_of<TD>(a.draft, b, t), lo, hi, threadIdx.x,
-                                      [&](const float (&v)[kVec<TD>], int, int) { soft_push(s, v, c); });
+            walk_row<TD, kStatThreads, 4>(y, lo, hi, threadIdx.x,
+                                          [&](const float (&v)[kVec<TD>], int, int) { soft_push(s, v, c); });
         else
-            walk_row<TT, kThreads, 4>(row_of<TT>(a.target, b, t), lo, hi, threadIdx.x,
-                                      [&](const float (&v)[kVec<TT>], int, int) { soft_push(s, v, c); });
-        s = block_soft<kThreads>(s, c, red);
-        if (threadIdx.x == 0)
-            p.stats[((b * 2 + drafted) * (a.G + 1) + t) * p.parts + part] = make_float2(s.m, s.s);
+            walk_row<TT, kStatThreads, 4>(x, lo, hi, threadIdx.x,
+                                          [&](const float (&v)[kVec<TT>], int, int) { soft_push(s, v, c); });
+        s = block_soft<kStatThreads>(s, c, red);
+        if (threadIdx.x == 0) p.stats[row * p.parts + part] = make_float2(s.m, s.s);
     }
-}
-
-__device__ __forceinline__ Soft row_stats(const Plan& p, int64_t b, int side, int64_t G, int64_t t,
-                                          float c) {
-    Soft s = soft_empty();
-    const float2* q = p.stats + ((b * 2 + side) * (G + 1) + t) * p.parts;
-    for (int k = 0; k < p.parts; ++k) s = soft_merge(s, {q[k].x, q[k].y}, c);
-    return s;
 }
 
 // log-probability of a logit, in 64 bits: what is decided by it are whole tokens
@@ -96,106 +113,190 @@ __device__ __forceinline__ double log_prob(float x, Soft s, const Scale& k) {
     return ((double)x - (double)s.m) * (double)k.inv_t - log((double)s.s);
 }
 
-template <class TT, class TD>
-__global__ __launch_bounds__(kThreads) void k_verify_draw(VerifyArgs a, Plan p) {
-    __shared__ int stop;
-    __shared__ uint64_t words[kThreads / kWave];
-    const int tid = threadIdx.x;
-    for (int64_t i = blockIdx.x; i < a.B * p.parts; i += gridDim.x) {
-        const int64_t b = i / p.parts;
-        const int part = (int)(i % p.parts);
-        const int64_t n = clamp_rows(a.lengths, b, a.G);
-        // the first draft that is refused
-        if (tid == 0) stop = (int)n;
-        __syncthreads();
-        for (int64_t t = tid; t < n; t += kThreads) {
-            const int z = a.tokens[b * a.G + t];
-            bool ok = false;
-            if (z >= 0 && z < a.V) {
-                const Soft s = row_stats(p, b, 0, a.G, t, a.scale.c);
-                const float x = to_f(row_of<TT>(a.target, b, t)[z]);
-                const float y = to_f(row_of<TD>(a.draft, b, t)[z]);
-                double lq;
-                if (a.draft_lse)
-                    lq = (double)y * (double)a.draft_scale.inv_t - (double)a.draft_lse[b * a.G + t];
-                else
-                    lq = log_prob(y, row_stats(p, b, 1, a.G, t, a.draft_scale.c), a.draft_scale);
-                if (x > -INFINITY) {
-                    const double lp = log_prob(x, s, a.scale);
-                    ok = y == -INFINITY || (double)a.uniforms[b * a.G + t] * exp(lq) < exp(lp);
-                }
-            }
-            if (!ok) atomicMin(&stop, (int)t);
+struct Tests {
+    Soft soft[2][kWave + 1];   // of the positions looked at: target, draft
+    float logp[kWave];
+    int stop;
+};
+
+// The first draft of [t0, t1), t1 - t0 <= 64, that is refused, or t1.  sh.soft then holds the
+// rows' statistics, the target's of position t1 too, and sh.logp the drafts' log-probabilities.
+template <int NT>
+__device__ int test_drafts(const VerifyArgs& a, const Plan& p, int64_t b, int64_t t0, int64_t t1,
+                           Tests& sh) {
+    const int tid = threadIdx.x, lane = tid % kWave, m = (int)(t1 - t0);
+    if (tid == 0) sh.stop = m;
+    const bool sums = !a.draft_lse;
+    for (int r = tid / kWave; r < m + 1 + (sums ? m : 0); r += NT / kWave) {
+        const int side = r > m, t = side ? r - m - 1 : r;
+        const float2 q = lane < p.parts ? p.stats[row_index(a, b, side, t0 + t) * p.parts + lane]
+                                        : make_float2(-FLT_MAX, 0.f);
+        const Soft s = wave_soft({q.x, q.y}, side ? a.draft_scale.c : a.scale.c);
+        if (lane == 0) sh.soft[side][t] = s;
+    }
+    __syncthreads();
+    if (tid < m) {
+        const int64_t t = t0 + tid;
+        const float x = p.logit[row_index(a, b, 0, t)], y = p.logit[row_index(a, b, 1, t)];
+        bool ok = false;
+        if (x > -INFINITY) {
+            const double lp = log_prob(x, sh.soft[0][tid], a.scale);
+            const double lq = sums ? log_prob(y, sh.soft[1][tid], a.draft_scale)
+                                   : (double)y * (double)a.draft_scale.inv_t -
+                                         (double)a.draft_lse[b * a.G + t];
+            ok = y == -INFINITY || (double)a.uniforms[b * a.G + t] * exp(lq) < exp(lp);
+            sh.logp[tid] = (float)lp;
         }
-        __syncthreads();
-        const int64_t at = stop;
+        if (!ok) atomicMin(&sh.stop, tid);
+    }
+    __syncthreads();
+    return sh.stop;
+}
+
+// Eight elements of a row
+template <class T>
+struct Eight {
+    Raw<T> r[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* at) {
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) r[h] = *(const Raw<T>*)(at + h * kVec<T>);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+            float u[kVec<T>];
+            unpack<T>(r[h], u);
+#pragma unroll
+            for (int k = 0; k < kVec<T>; ++k) v[h * kVec<T> + k] = u[k];
+        }
+    }
+};
+
+// Rates of the race: p or max(p - q, 0) of a token from its logits
+struct Race {
+    float mp, ip, cp;   // target: p = 2^((x - mp) cp) ip
+    float mq, iq, cq;   // draft
+    bool refused;
+};
+__device__ __forceinline__ uint64_t race_word(const Race& r, float x, float y, float e, int v) {
+#pragma clang fp contract(off)   // where p and q are the same number their difference is 0
+    const float p = exp2_((x - r.mp) * r.cp) * r.ip;
+    const float d = r.refused ? p - exp2_((y - r.mq) * r.cq) * r.iq : p;
+    // a token of positive d stands above all others, which run by their p
+    const float score = (d > 0.f ? d : p) / fmaxf(e, FLT_MIN);
+    const uint32_t key = (__float_as_uint(score) & 0x7fffffffu) | (d > 0.f ? 0x80000000u : 0u);
+    return (uint64_t)key << 32 | (uint32_t)~v;
+}
+
+__device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const uint64_t y = __shfl_xor((unsigned long long)x, o, kWave);
+        x = x > y ? x : y;
+    }
+    return x;
+}
+
+// One workgroup per (sequence, part of the race)
+template <class TT, class TD>
+__global__ __launch_bounds__(kDrawThreads) void k_verify_draw(VerifyArgs a, Plan p) {
+    __shared__ Tests sh;
+    __shared__ uint64_t words[kDrawThreads / kWave];
+    const int tid = threadIdx.x;
+    for (int64_t i = blockIdx.x; i < a.B * p.draw_parts; i += gridDim.x) {
+        const int64_t b = i / p.draw_parts;
+        const int part = (int)(i % p.draw_parts);
+        const int64_t n = clamp_rows(a.lengths, b, a.G);
+        int32_t* out = a.out + b * (a.G + 1);
+        float* logp = a.logp ? a.logp + b * (a.G + 1) : nullptr;
+        // the first draft that is refused; the sequence's first workgroup writes what is accepted
+        int64_t t0 = 0, at;
+        for (;; t0 += kWave) {
+            const int64_t t1 = min(t0 + kWave, n);
+            const int stop = test_drafts<kDrawThreads>(a, p, b, t0, t1, sh);
+            at = t0 + stop;
+            if (part == 0 && tid < stop) {
+                out[t0 + tid] = a.tokens[b * a.G + t0 + tid];
+                if (logp) logp[t0 + tid] = sh.logp[tid];
+            }
+            if (at < t1 || t1 == n) break;
+            __syncthreads();
+        }
         const bool refused = at < n;
+        if (part == 0) {
+            for (int64_t t = at + 1 + tid; t <= a.G; t += kDrawThreads) {
+                out[t] = -1;
+                if (logp) logp[t] = 0.f;
+            }
+            if (tid == 0) a.accepted[b] = (int32_t)at;
+        }
         // the race over the row that the next token is drawn from
         const TT* x = row_of<TT>(a.target, b, at);
         const TD* y = refused ? row_of<TD>(a.draft, b, at) : nullptr;
         const float* e = a.noise + b * a.V;
-        const Soft sp = row_stats(p, b, 0, a.G, at, a.scale.c);
-        const float ip = sp.s > 0.f ? 1.f / sp.s : 0.f, cp = a.scale.c, cq = a.draft_scale.c;
-        float mq = 0.f, iq = 0.f;
+        const Soft sp = sh.soft[0][at - t0];
+        Race race{sp.m, sp.s > 0.f ? 1.f / sp.s : 0.f, a.scale.c, 0.f, 0.f, a.draft_scale.c, refused};
         if (refused) {
             if (a.draft_lse) {
-                mq = a.draft_lse[b * a.G + at] / a.draft_scale.inv_t;
-                iq = 1.f;
+                race.mq = a.draft_lse[b * a.G + at] / a.draft_scale.inv_t;
+                race.iq = 1.f;
             } else {
-                const Soft sq = row_stats(p, b, 1, a.G, at, cq);
-                mq = sq.m;
-                iq = sq.s > 0.f ? 1.f / sq.s : 0.f;
+                const Soft sq = sh.soft[1][at - t0];
+                race.mq = sq.m;
+                race.iq = sq.s > 0.f ? 1.f / sq.s : 0.f;
             }
         }
         int lo, hi;
-        part_range(a.V, p.parts, part, &lo, &hi);
+        part_range(a.V, p.draw_parts, part, &lo, &hi);
         uint64_t best = 0;
-        for (int v = lo + tid; v < hi; v += kThreads) {
-#pragma clang fp contract(off)   // where p and q are the same number their difference is 0
-            const float pv = exp2_((to_f(x[v]) - sp.m) * cp) * ip;
-            const float r = refused ? pv - exp2_((to_f(y[v]) - mq) * cq) * iq : pv;
-            // a token of positive r stands above all others, which run by their p
-            const float rate = r > 0.f ? r : pv;
-            const float score = rate > 0.f ? rate / e[v] : 0.f;
-            const uint32_t key = (__float_as_uint(score) & 0x7fffffffu) | (r > 0.f ? 0x80000000u : 0u);
-            const uint64_t word = (uint64_t)key << 32 | (uint32_t)~v;
+        int v = lo + tid * 8;
+        for (; v + 8 <= hi; v += kDrawThreads * 8) {
+            Eight<TT> rx;
+            Eight<TD> ry{};
+            Eight<float> re;
+            rx.load(x + v);
+            if (refused) ry.load(y + v);
+            re.load(e + v);
+            float xv[8], yv[8], ev[8];
+            rx.get(xv);
+            ry.get(yv);
+            re.get(ev);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint64_t word = race_word(race, xv[k], yv[k], ev[k], v + k);
+                best = best > word ? best : word;
+            }
+        }
+        for (; v < hi; ++v) {   // the thread that holds the part's last few
+            const uint64_t word =
+                race_word(race, to_f(x[v]), refused ? to_f(y[v]) : 0.f, e[v], v);
             best = best > word ? best : word;
         }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            const uint64_t other = __shfl_xor((unsigned long long)best, o, kWave);
-            best = best > other ? best : other;
-        }
+        best = wave_max64(best);
         if (tid % kWave == 0) words[tid / kWave] = best;
         __syncthreads();
         if (tid == 0) {
-            for (int w = 1; w < kThreads / kWave; ++w) best = best > words[w] ? best : words[w];
-            atomicMax((unsigned long long*)&p.best[b], (unsigned long long)best);
-            __threadfence();
-            stop = atomicSub(&p.left[b], 1) == 1 ? 1 : 0;
-        }
-        __syncthreads();
-        if (stop) {   // the last part to arrive writes what is emitted
-            __threadfence();
-            const uint64_t w =
-                __hip_atomic_load(&p.best[b], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            const int token = (int)~(uint32_t)w;
-            for (int64_t t = tid; t <= a.G; t += kThreads) {
-                const int z = t < at ? a.tokens[b * a.G + t] : t == at ? token : -1;
-                a.out[b * (a.G + 1) + t] = z;
-                if (!a.logp) continue;
-                float lp = 0.f;
-                if (t <= at) {
-                    const Soft s = row_stats(p, b, 0, a.G, t, a.scale.c);
-                    lp = s.s > 0.f
-                             ? (float)log_prob(to_f(row_of<TT>(a.target, b, t)[z]), s, a.scale)
-                             : -INFINITY;
-                }
-                a.logp[b * (a.G + 1) + t] = lp;
+            for (int w = 1; w < kDrawThreads / kWave; ++w) best = best > words[w] ? best : words[w];
+            bool mine = true;
+            if (p.draw_parts > 1) {
+                // The last part to arrive writes the winner.  All that the parts share are these
+                // two words, both touched by atomics alone, so no fence (which would write back
+                // and drop a whole L2) is needed: the count goes down once the maximum's old
+                // value is here, that is, once the maximum is done.
+                const unsigned long long old =
+                    atomicMax((unsigned long long*)&p.best[b], (unsigned long long)best);
+                asm volatile("" ::"v"(old) : "memory");
+                mine = atomicSub(&p.left[b], 1) == 1;
+                if (mine) best = atomicMax((unsigned long long*)&p.best[b], 0ull);
             }
-            if (tid == 0) a.accepted[b] = (int32_t)at;
+            if (mine) {
+                const int token = (int)~(uint32_t)best;
+                out[at] = token;
+                if (logp)
+                    logp[at] = sp.s > 0.f ? (float)log_prob(to_f(x[token]), sp, a.scale) : -INFINITY;
+            }
         }
-        __syncthreads();
+        __syncthreads();   // sh and words are free for the next part
     }
 }
 
@@ -210,8 +311,9 @@ hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
             using TT = decltype(t);
             using TD = decltype(d);
             k_verify_stats<TT, TD>
-                <<<row_grid(a.B * (2 * a.G + 1) * p.parts, kThreads), kThreads, 0, s>>>(a, p);
-            k_verify_draw<TT, TD><<<row_grid(a.B * p.parts, kThreads), kThreads, 0, s>>>(a, p);
+                <<<row_grid(a.B * (2 * a.G + 1) * p.parts, kStatThreads), kStatThreads, 0, s>>>(a, p);
+            k_verify_draw<TT, TD>
+                <<<row_grid(a.B * p.draw_parts, kDrawThreads), kDrawThreads, 0, s>>>(a, p);
         });
     });
     return hipGetLastError();
