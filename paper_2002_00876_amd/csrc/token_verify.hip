@@ -18,8 +18,14 @@ namespace {
 
 constexpr int kStatThreads = 256;
 constexpr int kDrawThreads = 512;
+constexpr int kSmallThreads = 1024;
+constexpr int kSmallElems = 4096;   // elements a wave, up to which one workgroup takes a sequence
 constexpr int kMaxParts = kWave;   // parts of a row: one a lane when they are joined
 constexpr int kMinPart = 2048;     // elements of a part: 8 a thread
+constexpr int kMaxGroups = 8;      // launches that the positions are divided among
+constexpr int kAlive = 0x7fffffff;
+constexpr double kApartElems = 8e6;   // elements of a position's rows from which it has a launch
+constexpr int kStatParts = 2048, kDrawParts = 1024;   // workgroups that fill the chip
 
 // Parts of a row: enough workgroups to fill the chip where the rows are few
 inline int parts_of(int64_t rows, int64_t V, int64_t want) {
@@ -38,16 +44,19 @@ __device__ __forceinline__ void part_range(int V, int parts, int part, int* lo, 
 
 struct Plan {
     int parts, draw_parts;
+    bool apart;       // the positions are divided among launches
     float2* stats;    // [B][2][G + 1][parts]: target's, draft's maximum and sum
     float* logit;     // [B][2][G + 1]: their logits of the draft
     uint64_t* best;   // [B] the race's largest word so far
     int32_t* left;    // [B] parts of the race that have not arrived
+    int32_t* stop;    // [kMaxGroups][B] first draft refused before the group's, or kAlive
     size_t bytes;
 };
 inline Plan plan_of(int64_t B, int64_t G, int64_t V, void* ws) {
     Plan p;
-    p.parts = parts_of(B * (2 * G + 1), V, 4096);
-    p.draw_parts = parts_of(B, V, 1024);
+    p.apart = (double)B * V >= kApartElems;
+    p.parts = parts_of(p.apart ? 2 * B : B * (2 * G + 1), V, kStatParts);
+    p.draw_parts = parts_of(B, V, kDrawParts);
     char* base = (char*)ws;
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -60,6 +69,7 @@ inline Plan plan_of(int64_t B, int64_t G, int64_t V, void* ws) {
     p.logit = (float*)take(rows * sizeof(float));
     p.best = (uint64_t*)take((size_t)B * sizeof(uint64_t));
     p.left = (int32_t*)take((size_t)B * sizeof(int32_t));
+    p.stop = (int32_t*)take((size_t)B * kMaxGroups * sizeof(int32_t));
     p.bytes = off;
     return p;
 }
@@ -67,23 +77,102 @@ __device__ __forceinline__ int64_t row_index(const VerifyArgs& a, int64_t b, int
     return (b * 2 + side) * (a.G + 1) + t;
 }
 
-// One workgroup per (sequence, side and position, part): maximum and sum of a part of a row
+__device__ __forceinline__ float log_prob(float x, Soft s, const Scale& k) {
+    return (x - s.m) * k.inv_t - logf(s.s);
+}
+
+// 2^((x - m) c) with the product's rounding made good: the hardware's exponential (2^-23) is
+// what is left of the error, also far below the maximum
+__device__ __forceinline__ float numerator(float x, float m, float c) {
+    const float d = x - m, e = d * c;
+    return exp2_(e) * fmaf(fmaf(d, c, -e), 0.69314718f, 1.f);
+}
+
+// Whether a draft of target's logit x and draft's y is accepted, and its log-probability.
+// u q < p without a division: u e_q s_p < e_p s_q, the products in 64 bits.
+__device__ __forceinline__ bool accepts(const VerifyArgs& a, float x, float y, float u, float lse,
+                                        Soft sp, Soft sq, float* logp) {
+    *logp = 0.f;
+    if (!(x > -INFINITY)) return false;
+    *logp = log_prob(x, sp, a.scale);
+    if (y == -INFINITY) return true;
+    const float c = a.draft_scale.c;
+    const double q = a.draft_lse ? numerator(y, lse / a.draft_scale.inv_t, c) : numerator(y, sq.m, c);
+    return (double)u * q * (double)sp.s <
+           (double)numerator(x, sp.m, a.scale.c) * (a.draft_lse ? 1.0 : (double)sq.s);
+}
+
+struct Tests {
+    Soft soft[2][kWave + 1];   // of the positions looked at: target, draft
+    float logp[kWave];
+    int stop;
+};
+
+// The first draft of [t0, t1), t1 - t0 <= 64, that is refused, or t1.  sh.soft then holds the
+// rows' statistics, the target's of position t1 too, and sh.logp the drafts' log-probabilities.
+template <int NT>
+__device__ int test_drafts(const VerifyArgs& a, const Plan& p, int64_t b, int64_t t0, int64_t t1,
+                           Tests& sh) {
+    const int tid = threadIdx.x, lane = tid % kWave, m = (int)(t1 - t0);
+    if (tid == 0) sh.stop = m;
+    const bool sums = !a.draft_lse;
+    float x = 0.f, y = 0.f, u = 0.f, l = 0.f;
+    if (tid < m) {
+        x = p.logit[row_index(a, b, 0, t0 + tid)];
+        y = p.logit[row_index(a, b, 1, t0 + tid)];
+        u = a.uniforms[b * a.G + t0 + tid];
+        if (!sums) l = a.draft_lse[b * a.G + t0 + tid];
+    }
+    for (int r = tid / kWave; r < m + 1 + (sums ? m : 0); r += NT / kWave) {
+        const int side = r > m, t = side ? r - m - 1 : r;
+        const float2 q = lane < p.parts ? p.stats[row_index(a, b, side, t0 + t) * p.parts + lane]
+                                        : make_float2(-FLT_MAX, 0.f);
+        const Soft s = wave_soft({q.x, q.y}, side ? a.draft_scale.c : a.scale.c);
+        if (lane == 0) sh.soft[side][t] = s;
+    }
+    __syncthreads();
+    if (tid < m) {
+        float lp;
+        if (!accepts(a, x, y, u, l, sh.soft[0][tid], sh.soft[1][tid], &lp)) atomicMin(&sh.stop, tid);
+        sh.logp[tid] = lp;
+    }
+    __syncthreads();
+    return sh.stop;
+}
+
+// One workgroup per (sequence, position of [t0, t1) and side, part): maximum and sum of a part of
+// a row.  The positions of a large call are divided among launches, of which `group` counts the
+// earlier ones: the last of those began at position `before`, and sequences that have had a draft
+// refused by then are done.
 template <class TT, class TD>
-__global__ __launch_bounds__(kStatThreads) void k_verify_stats(VerifyArgs a, Plan p) {
+__global__ __launch_bounds__(kStatThreads) void k_verify_stats(VerifyArgs a, Plan p, int64_t before,
+                                                               int64_t t0, int64_t t1, int group) {
     __shared__ float2 red[kStatThreads / kWave];
-    const int64_t per = (int64_t)p.parts * (2 * a.G + 1);
-    for (int64_t i = blockIdx.x; i < per * a.B; i += gridDim.x) {
-        const int64_t b = i / per;
-        const int part = (int)(i % p.parts);
-        const int64_t r = i % per / p.parts;
-        const bool drafted = r > a.G;
-        const int64_t t = drafted ? r - a.G - 1 : r;
+    __shared__ Tests sh;
+    // 32-bit divisions: parts * rows stay below 2^32 (a row has parts only where rows are few)
+    const uint32_t width = 2 * (uint32_t)(t1 - t0), items = (uint32_t)(p.parts * a.B * width);
+    for (uint32_t i = blockIdx.x; i < items; i += gridDim.x) {
+        const uint32_t row_at = i / (uint32_t)p.parts, part = i % (uint32_t)p.parts;
+        const int64_t b = row_at / width;
+        const uint32_t r = row_at % width;
+        const int64_t t = t0 + r / 2;
+        const bool drafted = r & 1, first = r == 0 && part == 0;
         const int64_t n = clamp_rows(a.lengths, b, a.G);
-        if (r == 0 && part == 0 && threadIdx.x == 0) {
+        if (group == 0 && first && threadIdx.x == 0) {
             p.best[b] = 0;
             p.left[b] = p.draw_parts;
         }
         if (t >= n + (drafted ? 0 : 1)) continue;
+        if (group > 0) {
+            int stop = group > 1 ? p.stop[(group - 1) * a.B + b] : kAlive;
+            if (stop == kAlive) {   // t0 <= n: all of the last launch's positions have drafts
+                const int k = test_drafts<kStatThreads>(a, p, b, before, t0, sh);
+                if (before + k < t0) stop = (int)(before + k);
+                __syncthreads();
+            }
+            if (first && threadIdx.x == 0) p.stop[group * a.B + b] = stop;
+            if (stop != kAlive) continue;
+        }
         const TT* x = row_of<TT>(a.target, b, t);
         const TD* y = drafted ? row_of<TD>(a.draft, b, t) : nullptr;
         const int64_t row = row_index(a, b, drafted, t);
@@ -106,51 +195,6 @@ __global__ __launch_bounds__(kStatThreads) void k_verify_stats(VerifyArgs a, Pla
         s = block_soft<kStatThreads>(s, c, red);
         if (threadIdx.x == 0) p.stats[row * p.parts + part] = make_float2(s.m, s.s);
     }
-}
-
-// log-probability of a logit, in 64 bits: what is decided by it are whole tokens
-__device__ __forceinline__ double log_prob(float x, Soft s, const Scale& k) {
-    return ((double)x - (double)s.m) * (double)k.inv_t - log((double)s.s);
-}
-
-struct Tests {
-    Soft soft[2][kWave + 1];   // of the positions looked at: target, draft
-    float logp[kWave];
-    int stop;
-};
-
-// The first draft of [t0, t1), t1 - t0 <= 64, that is refused, or t1.  sh.soft then holds the
-// rows' statistics, the target's of position t1 too, and sh.logp the drafts' log-probabilities.
-template <int NT>
-__device__ int test_drafts(const VerifyArgs& a, const Plan& p, int64_t b, int64_t t0, int64_t t1,
-                           Tests& sh) {
-    const int tid = threadIdx.x, lane = tid % kWave, m = (int)(t1 - t0);
-    if (tid == 0) sh.stop = m;
-    const bool sums = !a.draft_lse;
-    for (int r = tid / kWave; r < m + 1 + (sums ? m : 0); r += NT / kWave) {
-        const int side = r > m, t = side ? r - m - 1 : r;
-        const float2 q = lane < p.parts ? p.stats[row_index(a, b, side, t0 + t) * p.parts + lane]
-                                        : make_float2(-FLT_MAX, 0.f);
-        const Soft s = wave_soft({q.x, q.y}, side ? a.draft_scale.c : a.scale.c);
-        if (lane == 0) sh.soft[side][t] = s;
-    }
-    __syncthreads();
-    if (tid < m) {
-        const int64_t t = t0 + tid;
-        const float x = p.logit[row_index(a, b, 0, t)], y = p.logit[row_index(a, b, 1, t)];
-        bool ok = false;
-        if (x > -INFINITY) {
-            const double lp = log_prob(x, sh.soft[0][tid], a.scale);
-            const double lq = sums ? log_prob(y, sh.soft[1][tid], a.draft_scale)
-                                   : (double)y * (double)a.draft_scale.inv_t -
-                                         (double)a.draft_lse[b * a.G + t];
-            ok = y == -INFINITY || (double)a.uniforms[b * a.G + t] * exp(lq) < exp(lp);
-            sh.logp[tid] = (float)lp;
-        }
-        if (!ok) atomicMin(&sh.stop, tid);
-    }
-    __syncthreads();
-    return sh.stop;
 }
 
 // Eight elements of a row
@@ -178,6 +222,18 @@ struct Race {
     float mq, iq, cq;   // draft
     bool refused;
 };
+__device__ __forceinline__ Race race_of(const VerifyArgs& a, int64_t b, int64_t at, bool refused,
+                                        Soft sp, Soft sq) {
+    Race r{sp.m, sp.s > 0.f ? 1.f / sp.s : 0.f, a.scale.c, 0.f, 0.f, a.draft_scale.c, refused};
+    if (refused && a.draft_lse) {
+        r.mq = a.draft_lse[b * a.G + at] / a.draft_scale.inv_t;
+        r.iq = 1.f;
+    } else if (refused) {
+        r.mq = sq.m;
+        r.iq = sq.s > 0.f ? 1.f / sq.s : 0.f;
+    }
+    return r;
+}
 __device__ __forceinline__ uint64_t race_word(const Race& r, float x, float y, float e, int v) {
 #pragma clang fp contract(off)   // where p and q are the same number their difference is 0
     const float p = exp2_((x - r.mp) * r.cp) * r.ip;
@@ -203,9 +259,10 @@ __global__ __launch_bounds__(kDrawThreads) void k_verify_draw(VerifyArgs a, Plan
     __shared__ Tests sh;
     __shared__ uint64_t words[kDrawThreads / kWave];
     const int tid = threadIdx.x;
-    for (int64_t i = blockIdx.x; i < a.B * p.draw_parts; i += gridDim.x) {
-        const int64_t b = i / p.draw_parts;
-        const int part = (int)(i % p.draw_parts);
+    const uint32_t items = (uint32_t)(p.draw_parts * a.B);
+    for (uint32_t i = blockIdx.x; i < items; i += gridDim.x) {
+        const int64_t b = i / (uint32_t)p.draw_parts;
+        const int part = (int)(i % (uint32_t)p.draw_parts);
         const int64_t n = clamp_rows(a.lengths, b, a.G);
         int32_t* out = a.out + b * (a.G + 1);
         float* logp = a.logp ? a.logp + b * (a.G + 1) : nullptr;
@@ -235,17 +292,7 @@ __global__ __launch_bounds__(kDrawThreads) void k_verify_draw(VerifyArgs a, Plan
         const TD* y = refused ? row_of<TD>(a.draft, b, at) : nullptr;
         const float* e = a.noise + b * a.V;
         const Soft sp = sh.soft[0][at - t0];
-        Race race{sp.m, sp.s > 0.f ? 1.f / sp.s : 0.f, a.scale.c, 0.f, 0.f, a.draft_scale.c, refused};
-        if (refused) {
-            if (a.draft_lse) {
-                race.mq = a.draft_lse[b * a.G + at] / a.draft_scale.inv_t;
-                race.iq = 1.f;
-            } else {
-                const Soft sq = sh.soft[1][at - t0];
-                race.mq = sq.m;
-                race.iq = sq.s > 0.f ? 1.f / sq.s : 0.f;
-            }
-        }
+        const Race race = race_of(a, b, at, refused, sp, sh.soft[1][refused ? at - t0 : 0]);
         int lo, hi;
         part_range(a.V, p.draw_parts, part, &lo, &hi);
         uint64_t best = 0;
@@ -293,30 +340,143 @@ __global__ __launch_bounds__(kDrawThreads) void k_verify_draw(VerifyArgs a, Plan
                 const int token = (int)~(uint32_t)best;
                 out[at] = token;
                 if (logp)
-                    logp[at] = sp.s > 0.f ? (float)log_prob(to_f(x[token]), sp, a.scale) : -INFINITY;
+                    logp[at] = sp.s > 0.f ? log_prob(to_f(x[token]), sp, a.scale) : -INFINITY;
             }
         }
         __syncthreads();   // sh and words are free for the next part
     }
 }
 
+// A whole sequence by one workgroup, its rows by a wave each: vocabularies so small that a
+// second launch and the joining of parts would take longer than the rows do
+template <class TT, class TD>
+__global__ __launch_bounds__(kSmallThreads) void k_verify_small(VerifyArgs a) {
+    constexpr int kWaves = kSmallThreads / kWave;
+    __shared__ Tests sh;
+    __shared__ float logit[2][kWave];
+    __shared__ uint64_t words[kWaves];
+    const int tid = threadIdx.x, lane = tid % kWave;
+    for (int64_t b = blockIdx.x; b < a.B; b += gridDim.x) {
+        const int64_t n = clamp_rows(a.lengths, b, a.G);
+        int32_t* out = a.out + b * (a.G + 1);
+        float* logp = a.logp ? a.logp + b * (a.G + 1) : nullptr;
+        int64_t t0 = 0, at;
+        for (;; t0 += kWave) {
+            const int64_t t1 = min(t0 + kWave, n);
+            const int m = (int)(t1 - t0);
+            if (tid == 0) sh.stop = m;
+            for (int r = tid / kWave; r < 2 * m + 1; r += kWaves) {
+                const int side = r & 1, k = r / 2;
+                const int64_t t = t0 + k;
+                const TT* x = row_of<TT>(a.target, b, t);
+                const TD* y = side ? row_of<TD>(a.draft, b, t) : nullptr;
+                if (lane == 0 && k < m) {
+                    const int z = a.tokens[b * a.G + t];
+                    logit[side][k] = z < 0 || z >= a.V ? -INFINITY : side ? to_f(y[z]) : to_f(x[z]);
+                }
+                if (side && a.draft_lse) continue;
+                const float c = side ? a.draft_scale.c : a.scale.c;
+                Soft s = soft_empty();
+                if (side)
+                    walk_row<TD, kWave, 4>(y, 0, a.V, lane,
+                                           [&](const float (&v)[kVec<TD>], int, int) { soft_push(s, v, c); });
+                else
+                    walk_row<TT, kWave, 4>(x, 0, a.V, lane,
+                                           [&](const float (&v)[kVec<TT>], int, int) { soft_push(s, v, c); });
+                s = wave_soft(s, c);
+                if (lane == 0) sh.soft[side][k] = s;
+            }
+            __syncthreads();
+            if (tid < m) {
+                float lp;
+                const int64_t t = b * a.G + t0 + tid;
+                if (!accepts(a, logit[0][tid], logit[1][tid], a.uniforms[t],
+                             a.draft_lse ? a.draft_lse[t] : 0.f, sh.soft[0][tid], sh.soft[1][tid], &lp))
+                    atomicMin(&sh.stop, tid);
+                sh.logp[tid] = lp;
+            }
+            __syncthreads();
+            const int stop = sh.stop;
+            at = t0 + stop;
+            if (tid < stop) {
+                out[t0 + tid] = a.tokens[b * a.G + t0 + tid];
+                if (logp) logp[t0 + tid] = sh.logp[tid];
+            }
+            if (at < t1 || t1 == n) break;
+            __syncthreads();
+        }
+        for (int64_t t = at + 1 + tid; t <= a.G; t += kSmallThreads) {
+            out[t] = -1;
+            if (logp) logp[t] = 0.f;
+        }
+        const bool refused = at < n;
+        const TT* x = row_of<TT>(a.target, b, at);
+        const TD* y = refused ? row_of<TD>(a.draft, b, at) : nullptr;
+        const float* e = a.noise + b * a.V;
+        const Soft sp = sh.soft[0][at - t0];
+        const Race race = race_of(a, b, at, refused, sp, sh.soft[1][refused ? at - t0 : 0]);
+        uint64_t best = 0;
+        for (int v = tid; v < a.V; v += kSmallThreads) {
+            const uint64_t word = race_word(race, to_f(x[v]), refused ? to_f(y[v]) : 0.f, e[v], v);
+            best = best > word ? best : word;
+        }
+        best = wave_max64(best);
+        if (lane == 0) words[tid / kWave] = best;
+        __syncthreads();
+        if (tid == 0) {
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) best = best > words[w] ? best : words[w];
+            const int token = (int)~(uint32_t)best;
+            out[at] = token;
+            a.accepted[b] = (int32_t)at;
+            if (logp)
+                logp[at] = sp.s > 0.f ? log_prob(to_f(x[token]), sp, a.scale) : -INFINITY;
+        }
+        __syncthreads();   // sh and words are free for the next sequence
+    }
+}
+
+bool small(int64_t G, int64_t V) {
+    constexpr int kWaves = kSmallThreads / kWave;
+    return (2 * G + kWaves) / kWaves * V <= kSmallElems;
+}
+
 }  // namespace
 
-size_t verify_workspace(int64_t B, int64_t G, int64_t V) { return plan_of(B, G, V, nullptr).bytes; }
+size_t verify_workspace(int64_t B, int64_t G, int64_t V) {
+    return small(G, V) ? 0 : plan_of(B, G, V, nullptr).bytes;
+}
 
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
-    const Plan p = plan_of(a.B, a.G, a.V, a.ws);
+    hipError_t e = hipSuccess;
     with_type(a.target_dtype, [&](auto t) {
         with_type(a.draft_dtype, [&](auto d) {
             using TT = decltype(t);
             using TD = decltype(d);
-            k_verify_stats<TT, TD>
-                <<<row_grid(a.B * (2 * a.G + 1) * p.parts, kStatThreads), kStatThreads, 0, s>>>(a, p);
+            if (small(a.G, a.V)) {
+                k_verify_small<TT, TD><<<row_grid(a.B, kSmallThreads), kSmallThreads, 0, s>>>(a);
+                e = hipGetLastError();
+                return;
+            }
+            const Plan p = plan_of(a.B, a.G, a.V, a.ws);
+            // positions [0, 1), [1, 2), [2, 4), [4, 8) ... where a position is worth a launch
+            int64_t before = 0, t0 = 0;
+            for (int group = 0; t0 <= a.G; ++group) {
+                int64_t t1 = a.G + 1;
+                if (p.apart && group < kMaxGroups - 1) t1 = min(t1, t0 + (t0 > 1 ? t0 : 1));
+                k_verify_stats<TT, TD>
+                    <<<row_grid(a.B * 2 * (t1 - t0) * p.parts, kStatThreads), kStatThreads, 0, s>>>(
+                        a, p, before, t0, t1, group);
+                if ((e = hipGetLastError()) != hipSuccess) return;
+                before = t0;
+                t0 = t1;
+            }
             k_verify_draw<TT, TD>
                 <<<row_grid(a.B * p.draw_parts, kDrawThreads), kDrawThreads, 0, s>>>(a, p);
+            e = hipGetLastError();
         });
     });
-    return hipGetLastError();
+    return e;
 }
 
 }  // namespace tsc
