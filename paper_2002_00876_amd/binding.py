@@ -340,19 +340,14 @@ def _prep_small(x, name, dtype, shape, device):
     return x if x.is_contiguous() else x.contiguous()
 
 
-def _prep_out(x, name, dtype, shape, device):
-    x = _prep_small(x, name, dtype, shape, device)
-    return torch.empty(shape, dtype=dtype, device=device) if x is None else x
-
-
-def _prep_outs(out, names, dtypes, shapes, device):
-    for x, name in zip(out or (), names):
-        if x is not None and not x.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-    out = out or (None,) * len(names)
+def _check_outs(out, names, dtypes, shapes, device):
     if len(out) != len(names):
         raise ValueError(f"out must be ({', '.join(names)})")
-    return [_prep_out(*a, device) for a in zip(out, names, dtypes, shapes)]
+    for x, name, dtype, shape in zip(out, names, dtypes, shapes):
+        if x.dtype != dtype or x.shape != shape or x.device != device or not x.is_contiguous():
+            raise ValueError(f"{name} must be contiguous {dtype} {list(shape)} on the same device "
+                             "as the logits")
+    return out
 
 
 def token_workspace_bytes(op, B, N, V, K=1):
@@ -377,9 +372,14 @@ def top_logits(logits, K, lengths=None, temperature=1.0, out=None, ws=None):
     B, N, V = logits.shape
     dev = logits.device
     lengths = _prep_small(lengths, "lengths", torch.int32, (B,), dev)
-    values, indices, lse = _prep_outs(
-        out, ("values", "indices", "lse"), (logits.dtype, torch.int32, torch.float32),
-        ((B, N, K), (B, N, K), (B, N)), dev)
+    if out is None:
+        values = torch.empty((B, N, K), dtype=logits.dtype, device=dev)
+        indices = torch.empty((B, N, K), dtype=torch.int32, device=dev)
+        lse = torch.empty((B, N), dtype=torch.float32, device=dev)
+    else:
+        values, indices, lse = _check_outs(
+            out, ("values", "indices", "lse"), (logits.dtype, torch.int32, torch.float32),
+            ((B, N, K), (B, N, K), (B, N)), dev)
     w, nb = _token_workspace(TOKEN_TOP, B, N, V, K, dev, ws)
     _check(lib().ts_token_top(_ptr(logits), dtype, sb, sn, _ptr(lengths), B, N, V, K, temperature,
                               _ptr(values), _ptr(indices), _ptr(lse), _ptr(w), nb, _stream(dev)))
@@ -411,7 +411,10 @@ def distill(logits, top_values, top_indices, top_lse=None, lengths=None, tempera
     its slots; with it (its log-sum-exp [B, N] at this temperature) what they leave is one class.
     0 for padding."""
     head, kept, (B, N, V, K), dev = _prep_teacher(logits, top_values, top_indices, top_lse, lengths)
-    loss, = _prep_outs(None if out is None else (out,), ("loss",), (torch.float32,), ((B, N),), dev)
+    if out is None:
+        loss = torch.empty((B, N), dtype=torch.float32, device=dev)
+    else:
+        loss, = _check_outs((out,), ("loss",), (torch.float32,), ((B, N),), dev)
     w, nb = _token_workspace(TOKEN_DISTILL, B, N, V, K, dev, ws)
     _check(lib().ts_token_distill(*head, _ptr(kept[-1]), B, N, V, K, temperature, _ptr(loss),
                                   _ptr(w), nb, _stream(dev)))
@@ -424,8 +427,12 @@ def distill_grad(logits, top_values, top_indices, top_lse=None, lengths=None, we
     sum(weights * loss) by the logits, weights float32 [B, N] (None: all 1)."""
     head, kept, (B, N, V, K), dev = _prep_teacher(logits, top_values, top_indices, top_lse, lengths)
     weights = _prep_small(weights, "weights", torch.float32, (B, N), dev)
-    loss, grad = _prep_outs(out, ("loss", "grad"), (torch.float32, logits.dtype),
-                            ((B, N), (B, N, V)), dev)
+    if out is None:
+        loss = torch.empty((B, N), dtype=torch.float32, device=dev) if want_loss else None
+        grad = torch.empty((B, N, V), dtype=logits.dtype, device=dev)
+    else:
+        loss, grad = _check_outs(out, ("loss", "grad"), (torch.float32, logits.dtype),
+                                 ((B, N), (B, N, V)), dev)
     w, nb = _token_workspace(TOKEN_DISTILL_GRAD, B, N, V, K, dev, ws)
     _check(lib().ts_token_distill_grad(*head, _ptr(weights), _ptr(kept[-1]), B, N, V, K,
                                        temperature, _ptr(loss) if want_loss else None, _ptr(grad),
@@ -453,9 +460,14 @@ def verify(target, draft, tokens, uniforms, noise, lengths=None, draft_lse=None,
     noise = _prep_small(noise, "noise", torch.float32, (B, V), dev)
     draft_lse = _prep_small(draft_lse, "draft_lse", torch.float32, (B, G), dev)
     lengths = _prep_small(lengths, "lengths", torch.int32, (B,), dev)
-    emitted, accepted, logp = _prep_outs(
-        out, ("out", "accepted", "logp"), (torch.int32, torch.int32, torch.float32),
-        ((B, G + 1), (B,), (B, G + 1)), dev)
+    if out is None:
+        emitted = torch.empty((B, G + 1), dtype=torch.int32, device=dev)
+        accepted = torch.empty(B, dtype=torch.int32, device=dev)
+        logp = torch.empty((B, G + 1), dtype=torch.float32, device=dev)
+    else:
+        emitted, accepted, logp = _check_outs(
+            out, ("out", "accepted", "logp"), (torch.int32, torch.int32, torch.float32),
+            ((B, G + 1), (B,), (B, G + 1)), dev)
     w, nb = _token_workspace(TOKEN_VERIFY, B, G, V, 1, dev, ws)
     _check(lib().ts_token_verify(_ptr(target), dtype, sb, sn, _ptr(draft), ddtype, db, dn,
                                  _ptr(draft_lse), _ptr(tokens), _ptr(uniforms), _ptr(noise),

@@ -185,6 +185,49 @@ __device__ __forceinline__ float block_max(float x, float* red) {
     return m;
 }
 
+// The same for whole chunks of a row, at one fma, one exponential and one sum a logit: the
+// maximum is brought up to date once a chunk, and numerators are 2^(v c - r), r = m c rounded.
+// What r is rounded by is common to all numerators and goes into the sum when the pair is read
+// off (value()), so a numerator's exponent is rounded once, as a difference.  Rows whose maximum
+// lies beyond +-kFar have m c outside the floats: they are walked again, by soft_push.
+constexpr float kFar = 1e30f;
+struct ChunkSoft {
+    float m, r, s;
+    __device__ __forceinline__ void init(float c) { m = -kFar, r = m * c, s = 0.f; }
+    __device__ __forceinline__ void raise(float most, float c) {
+        if (most > m) {
+            const float r2 = most * c;
+            s *= exp2_(r - r2);
+            m = most;
+            r = r2;
+        }
+    }
+    template <int W>
+    __device__ __forceinline__ void push(const float (&v)[W], float c) {
+        float t[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) t[k] = exp2_(fmaf(v[k], c, -r));
+#pragma unroll
+        for (int d = W / 2; d > 0; d /= 2)
+#pragma unroll
+            for (int k = 0; k < d; ++k) t[k] += t[k + d];
+        s += t[0];
+    }
+    __device__ __forceinline__ Soft value(float c) const {
+        // 2^(v c - r) = 2^((v - m) c) 2^(m c - r)
+        return {s > 0.f ? m : -FLT_MAX, s * exp2_(-fmaf(m, c, -r))};
+    }
+};
+__device__ __forceinline__ bool far(float most) { return !(fabsf(most) <= kFar); }
+
+template <int W>
+__device__ __forceinline__ float max_of(const float (&v)[W]) {
+    float a = fmaxf(v[0], fmaxf(v[1], v[2]));
+    if constexpr (W == 4) return fmaxf(a, v[3]);
+    const float b = fmaxf(v[3], fmaxf(v[4], v[5]));
+    return fmaxf(a, fmaxf(b, fmaxf(v[6], v[7])));
+}
+
 // log sum exp(x / T) of a row; -inf where it has no finite logit
 __device__ __forceinline__ float soft_lse(Soft a, float inv_t) {
     return a.s > 0.f ? fmaf(a.m, inv_t, logf(a.s)) : -INFINITY;

@@ -5,13 +5,18 @@
 // different and their order is that of the result: larger logits first, equal ones by the
 // lowest index.
 //
-// One workgroup takes a row.  The first walk keeps every thread's largest key and the running
-// maximum and sum of the softmax.  A threshold that at least K of the threads' largest keys
-// reach is one that at least K logits reach; as the K largest rarely share threads, few more
-// do (of 1024 threads' maxima the 256th is reached by some 300 logits).  The second walk
-// collects the logits that reach it, and each of them finds its place among them by counting.
-// Where more reach it than the list holds -- many equal logits, or the largest all in a few
-// threads -- the threshold is raised by bisection over the whole row, and logits equal to the
+// A threshold that K logits reach is found, the logits that reach it go into a list in LDS, and
+// each of them finds its place there by counting the larger ones.
+//   Rows of up to 8192 logits are held in registers: the threshold is found by bisection over
+// all of them (k_top_short).
+//   Longer rows are read once (k_top).  The threshold is taken from maxima of groups of logits,
+// kU groups a thread: one that K groups' maxima reach is one that at least K logits reach, and as
+// the K largest logits rarely share groups (of 1024 groups' maxima the 256th is reached by some
+// 300 logits) few more do.  It is found from the first chunk of the row and again each time the
+// part of the row that has been read has doubled; in between, logits that reach the last one
+// are appended, some K more for each doubling, and what falls below the next one leaves the list.
+//   Where more reach it than the list holds -- many equal logits, or the largest all in a few
+// groups -- the threshold is raised by bisection over the whole row, and logits equal to the
 // last threshold are taken in the order of their indices.
 #include <hip/hip_runtime.h>
 
@@ -21,6 +26,7 @@ namespace tsc {
 namespace {
 
 constexpr int kCap = 1024;   // logits that the list holds
+constexpr int kU = 4;        // vectors of a chunk, and groups, a thread
 
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.0f);   // -0 + 0 = 0
@@ -33,43 +39,177 @@ __device__ __forceinline__ uint64_t word_of(uint32_t key, int index) {
     return (uint64_t)key << 32 | (uint32_t)~index;
 }
 
-template <int NT>
-__device__ __forceinline__ int block_count(bool x) {
-    if constexpr (NT == kWave) return __popcll(__ballot(x));
-    return __syncthreads_count(x);
-}
-template <int NT>
-__device__ __forceinline__ int block_sum_int(int x, int* red) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
-    if constexpr (NT == kWave) return x;
-    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = x;
-    __syncthreads();
-    int s = 0;
-#pragma unroll
-    for (int w = 0; w < NT / kWave; ++w) s += red[w];
-    __syncthreads();
-    return s;
-}
-
 struct TopShared {
     uint64_t list[kCap];
     float2 red[16];
-    int redi[16];
+    int redi[2][16];
     int n;
 };
 
-// Appends the row's logits whose keys reach lo to the list, as far as it holds them; sh.n is
-// their number
+// Number of the workgroup's keys that reach lo; `turn` alternates between calls, which makes
+// one barrier enough
+template <int NT, int J>
+__device__ __forceinline__ int count_keys(const uint32_t (&key)[J], uint32_t lo, int turn,
+                                          TopShared& sh) {
+    int c = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) c += __popcll(__ballot(key[j] >= lo));
+    if constexpr (NT == kWave) return c;
+    if (threadIdx.x % kWave == 0) sh.redi[turn & 1][threadIdx.x / kWave] = c;
+    __syncthreads();
+    c = 0;
+#pragma unroll
+    for (int w = 0; w < NT / kWave; ++w) c += sh.redi[turn & 1][w];
+    return c;
+}
+
+// A threshold in [lo, hi) that at least K of the keys reach, K / 4 + 8 more at most where the
+// keys allow it; lo where fewer than K reach any other.  hi: none reaches it.  count: how many
+// reach the result (K or more only if it is not lo).
+template <int NT, int J>
+__device__ uint32_t threshold(const uint32_t (&key)[J], int K, uint32_t lo, uint32_t hi, int* count,
+                              TopShared& sh) {
+    int turn = 0;
+    *count = 0x7fffffff;
+    while (hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        const int c = count_keys<NT, J>(key, mid, turn++, sh);
+        if (c >= K) {
+            lo = mid;
+            *count = c;
+            if (c <= K + K / 4 + 8) break;
+        } else {
+            hi = mid;
+        }
+    }
+    if constexpr (NT > kWave) __syncthreads();   // redi is free for the next search
+    return lo;
+}
+
+// The list's words each find their place among them
+template <class T, int NT>
+__device__ __forceinline__ void write_places(const TopArgs& a, uint32_t row, int n,
+                                             const TopShared& sh) {
+    T* values = (T*)a.values + (size_t)row * a.K;
+    int32_t* indices = a.indices + (size_t)row * a.K;
+    for (int i = threadIdx.x; i < n; i += NT) {
+        const uint64_t w = sh.list[i];
+        int place = 0, j = 0;
+        for (; j + 4 <= n; j += 4)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) place += sh.list[j + k] > w;
+        for (; j < n; ++j) place += sh.list[j] > w;
+        if (place < a.K) {
+            values[place] = from_f<T>(of_key((uint32_t)(w >> 32)));
+            indices[place] = (int32_t)~(uint32_t)w;
+        }
+    }
+}
+
+template <class T, int NT>
+__device__ __forceinline__ void write_padding(const TopArgs& a, uint32_t row) {
+    for (int k = threadIdx.x; k < a.K; k += NT) {
+        ((T*)a.values)[(size_t)row * a.K + k] = from_f<T>(-INFINITY);
+        a.indices[(size_t)row * a.K + k] = -1;
+    }
+    if (a.lse && threadIdx.x == 0) a.lse[row] = -INFINITY;
+}
+
+// Puts the threads' hits into the list in the order of (call, thread); have: the words in it
+template <int NT>
+__device__ __forceinline__ int append_ordered(bool hit, uint64_t word, int have, int most,
+                                              TopShared& sh) {
+    const uint64_t votes = __ballot(hit);
+    int before = 0, all = __popcll(votes);
+    if constexpr (NT > kWave) {
+        if (threadIdx.x % kWave == 0) sh.redi[0][threadIdx.x / kWave] = all;
+        __syncthreads();
+        all = 0;
+#pragma unroll
+        for (int w = 0; w < NT / kWave; ++w) {
+            if (w < (int)threadIdx.x / kWave) before += sh.redi[0][w];
+            all += sh.redi[0][w];
+        }
+        __syncthreads();
+    }
+    before += have + __popcll(votes & ((1ull << (threadIdx.x % kWave)) - 1));
+    if (hit && before < most) sh.list[before] = word;
+    return min(have + all, most);
+}
+
+// Rows of up to NT * J logits
+template <class T, int NT, int J>
+__global__ __launch_bounds__(NT) void k_top_short(TopArgs a) {
+    __shared__ TopShared sh;
+    const int tid = threadIdx.x, K = a.K, V = a.V;
+    const uint32_t rows = (uint32_t)(a.B * a.N), N = (uint32_t)a.N;
+    for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const uint32_t b = row / N, n = row % N;
+        if (n >= clamp_rows(a.lengths, b, N)) {
+            write_padding<T, NT>(a, row);
+            continue;
+        }
+        const T* x = row_of<T>(a.logits, b, n);
+        float v[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int e = j * NT + tid;
+            v[j] = e < V ? to_f(x[e]) : -INFINITY;
+        }
+        Soft soft = soft_empty();
+        uint32_t key[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            soft.m = fmaxf(soft.m, v[j]);
+            key[j] = j * NT + tid < V ? key_of(v[j]) : 0u;   // 0: below every logit's
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) soft.s += exp2_((v[j] - soft.m) * a.scale.c);
+        soft = block_soft<NT>(soft, a.scale.c, sh.red);
+        if (a.lse && tid == 0) a.lse[row] = soft_lse(soft, a.scale.inv_t);
+        int have = 0, c;
+        if (V <= kCap && V <= 2 * K + 64) {   // a search would leave out little
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (j * NT + tid < V) sh.list[j * NT + tid] = word_of(key[j], j * NT + tid);
+            have = V;
+        } else {
+            const uint32_t lo = threshold<NT, J>(key, K, 0, key_of(INFINITY) + 1, &c, sh);
+            const uint32_t first = c > kCap ? lo + 1 : lo;   // too many equal lo
+            if (tid == 0) sh.n = 0;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (key[j] >= first) sh.list[atomicAdd(&sh.n, 1)] = word_of(key[j], j * NT + tid);
+            __syncthreads();
+            have = sh.n;
+            if (c > kCap)
+                for (int j = 0; j < J && have < K; ++j) {
+                    uint32_t kj = key[0];
+#pragma unroll
+                    for (int i = 1; i < J; ++i) kj = i == j ? key[i] : kj;
+                    have = append_ordered<NT>(kj == lo, word_of(lo, j * NT + tid), have, K, sh);
+                }
+        }
+        __syncthreads();
+        write_places<T, NT>(a, row, have, sh);
+        __syncthreads();   // the list is free for the next row
+    }
+}
+
+// ---- longer rows ----
+
+// Appends the row's logits whose keys reach lo, that of a finite logit, to the list, as far as it
+// holds them; sh.n is their number
 template <class T, int NT>
 __device__ void collect(const T* row, int V, uint32_t lo, TopShared& sh) {
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
     const float least = of_key(lo);
-    walk_row<T, NT, 4>(row, 0, V, threadIdx.x, [&](const float* v, int at, int num) {
+    walk_row<T, NT, 4>(row, 0, V, threadIdx.x, [&](const float (&v)[kVec<T>], int at, int num) {
 #pragma unroll
         for (int k = 0; k < kVec<T>; ++k)
-            if (k < num && (lo == 0 || v[k] >= least)) {
+            if (k < num && v[k] >= least) {
                 const int i = atomicAdd(&sh.n, 1);
                 if (i < kCap) sh.list[i] = word_of(key_of(v[k]), at + k);
             }
@@ -81,43 +221,45 @@ template <class T, int NT>
 __device__ int count_row(const T* row, int V, uint32_t lo, TopShared& sh) {
     int c = 0;
     const float least = of_key(lo);
-    walk_row<T, NT, 4>(row, 0, V, threadIdx.x, [&](const float* v, int, int num) {
+    walk_row<T, NT, 4>(row, 0, V, threadIdx.x, [&](const float (&v)[kVec<T>], int, int num) {
 #pragma unroll
         for (int k = 0; k < kVec<T>; ++k) c += k < num && v[k] >= least;
     });
-    return block_sum_int<NT>(c, sh.redi);
-}
-
-// The largest threshold found that K of the threads' keys reach, 0 where fewer than K threads
-// have one
-template <int NT>
-__device__ uint32_t threshold(uint32_t key, int K) {
-    uint32_t lo = 0, hi = 0xffffffffu;
-    while (hi - lo > 1) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        const int c = block_count<NT>(key >= mid);
-        if (c >= K) {
-            lo = mid;
-            if (c <= K + K / 4) break;
-        } else {
-            hi = mid;
-        }
-    }
-    return lo;
-}
-
-// Leaves in the list the row's K largest words and perhaps others, and in sh.n their number
-template <class T, int NT>
-__device__ void select(const T* row, int V, int K, uint32_t lo, TopShared& sh) {
-    collect<T, NT>(row, V, lo, sh);
-    const int n = sh.n;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) c += __shfl_xor(c, o, kWave);
+    if (threadIdx.x % kWave == 0) sh.redi[0][threadIdx.x / kWave] = c;
     __syncthreads();
-    if (n <= kCap) return;
-    // more than the list holds reach lo, and none reaches the key of +inf's successor
+    c = 0;
+#pragma unroll
+    for (int w = 0; w < NT / kWave; ++w) c += sh.redi[0][w];
+    __syncthreads();
+    return c;
+}
+
+// The logits equal to the one of key `tie`, in the order of their indices, until the list has
+// K words
+template <class T, int NT>
+__device__ int append_equal(const T* row, int V, int K, uint32_t tie, int have, TopShared& sh) {
+    for (int base = 0; base < V && have < K; base += NT) {
+        const int e = base + (int)threadIdx.x;
+        const bool hit = e < V && key_of(to_f(row[e])) == tie;
+        have = append_ordered<NT>(hit, word_of(tie, e), have, K, sh);
+    }
+    __syncthreads();
+    return have;
+}
+
+// The list from the row itself, where more logits than it holds reach lo.  Leaves the row's K
+// largest words in it and perhaps others; returns their number.
+template <class T, int NT>
+__device__ int select_again(const T* row, int V, int K, uint32_t lo, TopShared& sh) {
     uint32_t hi = key_of(INFINITY) + 1;
-    int c = n;
+    collect<T, NT>(row, V, lo, sh);
+    int c = sh.n;
+    __syncthreads();
+    if (c <= kCap) return c;
+    uint32_t mid = lo + 1;   // the usual reason: many that equal lo
     while (hi - lo > 1 && c > kCap) {
-        const uint32_t mid = lo + (hi - lo) / 2;
         const int m = count_row<T, NT>(row, V, mid, sh);
         if (m >= K) {
             lo = mid;
@@ -125,75 +267,131 @@ __device__ void select(const T* row, int V, int K, uint32_t lo, TopShared& sh) {
         } else {
             hi = mid;
         }
+        mid = lo + (hi - lo) / 2;
     }
-    if (c <= kCap) {
-        collect<T, NT>(row, V, lo, sh);
-        return;
-    }
-    // fewer than K logits lie above lo, and more equal it than the list holds: the first ones
-    collect<T, NT>(row, V, hi, sh);
-    int have = sh.n;
+    collect<T, NT>(row, V, c <= kCap ? lo : hi, sh);
+    const int have = sh.n;
     __syncthreads();
-    for (int base = 0; base < V && have < K; base += NT) {
-        const int e = base + (int)threadIdx.x;
-        const bool hit = e < V && key_of(to_f(row[e])) == lo;
-        const uint64_t votes = __ballot(hit);
-        if (threadIdx.x % kWave == 0) sh.redi[threadIdx.x / kWave] = __popcll(votes);
-        __syncthreads();
-        int before = 0, all = 0;
-        for (int w = 0; w < NT / kWave; ++w) {
-            if (w < (int)threadIdx.x / kWave) before += sh.redi[w];
-            all += sh.redi[w];
-        }
-        before += __popcll(votes & ((1ull << (threadIdx.x % kWave)) - 1));
-        if (hit && have + before < K) sh.list[have + before] = word_of(lo, e);
-        have += all;
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) sh.n = have < K ? have : K;
-    __syncthreads();
+    return c <= kCap ? have : append_equal<T, NT>(row, V, K, lo, have, sh);
 }
 
 template <class T, int NT>
 __global__ __launch_bounds__(NT) void k_top(TopArgs a) {
     __shared__ TopShared sh;
-    const int tid = threadIdx.x, K = a.K;
-    for (int64_t row = blockIdx.x; row < a.B * a.N; row += gridDim.x) {
-        const int64_t b = row / a.N, n = row % a.N;
-        T* values = (T*)a.values + row * K;
-        int32_t* indices = a.indices + row * K;
-        if (n >= clamp_rows(a.lengths, b, a.N)) {
-            for (int k = tid; k < K; k += NT) {
-                values[k] = from_f<T>(-INFINITY);
-                indices[k] = -1;
-            }
-            if (a.lse && tid == 0) a.lse[row] = -INFINITY;
+    constexpr int W = kVec<T>;
+    const int tid = threadIdx.x, K = a.K, V = a.V, nv = V / W;
+    const float c = a.scale.c;
+    const uint32_t rows = (uint32_t)(a.B * a.N), N = (uint32_t)a.N;
+    for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const uint32_t b = row / N, n = row % N;
+        if (n >= clamp_rows(a.lengths, b, N)) {
+            write_padding<T, NT>(a, row);
             continue;
         }
         const T* x = row_of<T>(a.logits, b, n);
-        Soft soft = soft_empty();
-        float most = -INFINITY;
-        bool any = false;
-        walk_row<T, NT, 4>(x, 0, a.V, tid, [&](const float (&v)[kVec<T>], int, int) {
-            soft_push(soft, v, a.scale.c);
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+        ChunkSoft soft;
+        soft.init(c);
+        float group[kU];
 #pragma unroll
-            for (int k = 0; k < kVec<T>; ++k) most = fmaxf(most, v[k]);
-            any = true;
-        });
-        soft = block_soft<NT>(soft, a.scale.c, sh.red);
-        if (a.lse && tid == 0) a.lse[row] = soft_lse(soft, a.scale.inv_t);
-        const uint32_t lo = a.V <= 128 ? 0 : threshold<NT>(any ? key_of(most) : 0, K);
-        select<T, NT>(x, a.V, K, lo, sh);
-        const int c = sh.n;
-        for (int i = tid; i < c; i += NT) {
-            const uint64_t w = sh.list[i];
-            int place = 0;
-            for (int j = 0; j < c; ++j) place += sh.list[j] > w;
-            if (place < K) {
-                values[place] = from_f<T>(of_key((uint32_t)(w >> 32)));
-                indices[place] = (int32_t)~(uint32_t)w;
+        for (int u = 0; u < kU; ++u) group[u] = -INFINITY;
+        float least = -FLT_MAX;        // the threshold: -inf is none of the K largest before
+        uint32_t lo = key_of(least);   // every finite logit is
+        bool lost = false;             // the list overflowed
+        auto append = [&](float v, int e) {
+            const int i = atomicAdd(&sh.n, 1);
+            if (i < kCap) sh.list[i] = word_of(key_of(v), e);
+        };
+        // the groups' maxima raise the threshold; what falls below it leaves the list
+        auto raise = [&](bool first) {
+            uint32_t key[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u) key[u] = key_of(group[u]);
+            int reach;
+            lo = threshold<NT, kU>(key, K, lo, key_of(INFINITY) + 1, &reach, sh);
+            least = of_key(lo);
+            if (first) return;
+            __syncthreads();
+            const int have = sh.n;
+            lost |= have > kCap;
+            uint64_t keep[kCap / NT];
+#pragma unroll
+            for (int j = 0; j < kCap / NT; ++j) {
+                const int i = j * NT + tid;
+                keep[j] = i < have ? sh.list[i] : 0;
             }
+            __syncthreads();
+            if (tid == 0) sh.n = 0;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < kCap / NT; ++j)
+                if (j * NT + tid < have && (uint32_t)(keep[j] >> 32) >= lo)
+                    sh.list[atomicAdd(&sh.n, 1)] = keep[j];
+            __syncthreads();
+        };
+        const int chunks = (nv + NT * kU - 1) / (NT * kU);
+        for (int ch = 0; ch < chunks; ++ch) {
+            const int i0 = ch * NT * kU + tid;
+            Raw<T> r[kU];
+            float most = -INFINITY;
+            const bool whole = (ch + 1) * NT * kU <= nv;
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                if (whole || i0 + u * NT < nv) r[u] = *(const Raw<T>*)(x + (size_t)(i0 + u * NT) * W);
+            float top[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                top[u] = -INFINITY;
+                if (whole || i0 + u * NT < nv) {
+                    float v[W];
+                    unpack<T>(r[u], v);
+                    top[u] = max_of(v);
+                }
+                group[u] = fmaxf(group[u], top[u]);
+                most = fmaxf(most, top[u]);
+            }
+            soft.raise(most, c);
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                if (whole || i0 + u * NT < nv) {
+                    float v[W];
+                    unpack<T>(r[u], v);
+                    soft.push(v, c);
+                }
+            if ((ch & (ch + 1)) == 0) raise(ch == 0);   // after chunks 1, 2, 4, 8 ...
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                if ((whole || i0 + u * NT < nv) && top[u] >= least) {
+                    float v[W];
+                    unpack<T>(r[u], v);
+#pragma unroll
+                    for (int k = 0; k < W; ++k)
+                        if (v[k] >= least) append(v[k], (i0 + u * NT) * W + k);
+                }
         }
+        const int e = nv * W + tid;   // the row's last few logits
+        if (e < V) {
+            const float v = to_f(x[e]);
+            float one[1] = {v};
+            soft.raise(v, c);
+            soft.push(one, c);
+            group[0] = fmaxf(group[0], v);
+            if (v >= least) append(v, e);
+        }
+        const float mine = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
+        raise(false);
+        Soft all = block_soft<NT>(soft.value(c), c, sh.red);
+        if (far(block_max<NT>(mine, (float*)sh.red))) {
+            Soft again = soft_empty();
+            walk_row<T, NT, 4>(x, 0, V, tid,
+                               [&](const float (&v)[W], int, int) { soft_push(again, v, c); });
+            all = block_soft<NT>(again, c, sh.red);
+        }
+        if (a.lse && tid == 0) a.lse[row] = soft_lse(all, a.scale.inv_t);
+        int have = lost ? select_again<T, NT>(x, V, K, lo, sh) : sh.n;
+        if (have < K) have = append_equal<T, NT>(x, V, K, key_of(-INFINITY), have, sh);
+        write_places<T, NT>(a, row, have, sh);
         __syncthreads();   // the list is free for the next row
     }
 }
@@ -206,12 +404,19 @@ hipError_t launch_top(const TopArgs& a, hipStream_t s) {
     with_type(a.dtype, [&](auto t) {
         using T = decltype(t);
         const int64_t rows = a.B * a.N;
-        if (a.V <= 512)
-            k_top<T, 64><<<row_grid(rows, 64), 64, 0, s>>>(a);
+        const unsigned g1 = row_grid(rows, 64), g4 = row_grid(rows, 256);
+        if (a.V <= 64)
+            k_top_short<T, 64, 1><<<g1, 64, 0, s>>>(a);
+        else if (a.V <= 256)
+            k_top_short<T, 64, 4><<<g1, 64, 0, s>>>(a);
+        else if (a.V <= 1024)
+            k_top_short<T, 64, 16><<<g1, 64, 0, s>>>(a);
+        else if (a.V <= 4096)
+            k_top_short<T, 256, 16><<<g4, 256, 0, s>>>(a);
         else if (a.V <= 8192)
-            k_top<T, 256><<<row_grid(rows, 256), 256, 0, s>>>(a);
+            k_top_short<T, 256, 32><<<g4, 256, 0, s>>>(a);
         else
-            k_top<T, 1024><<<row_grid(rows, 1024), 1024, 0, s>>>(a);
+            k_top<T, 256><<<g4, 256, 0, s>>>(a);
     });
     return hipGetLastError();
 }
