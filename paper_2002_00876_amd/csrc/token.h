@@ -223,9 +223,12 @@ __device__ __forceinline__ bool far(float most) { return !(fabsf(most) <= kFar);
 template <int W>
 __device__ __forceinline__ float max_of(const float (&v)[W]) {
     float a = fmaxf(v[0], fmaxf(v[1], v[2]));
-    if constexpr (W == 4) return fmaxf(a, v[3]);
-    const float b = fmaxf(v[3], fmaxf(v[4], v[5]));
-    return fmaxf(a, fmaxf(b, fmaxf(v[6], v[7])));
+    if constexpr (W == 4) {
+        return fmaxf(a, v[3]);
+    } else {
+        const float b = fmaxf(v[3], fmaxf(v[4], v[5]));
+        return fmaxf(a, fmaxf(b, fmaxf(v[6], v[7])));
+    }
 }
 
 // log sum exp(x / T) of a row; -inf where it has no finite logit

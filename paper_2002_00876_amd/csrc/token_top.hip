@@ -9,12 +9,14 @@
 // each of them finds its place there by counting the larger ones.
 //   Rows of up to 8192 logits are held in registers: the threshold is found by bisection over
 // all of them (k_top_short).
-//   Longer rows are read once (k_top).  The threshold is taken from maxima of groups of logits,
-// kU groups a thread: one that K groups' maxima reach is one that at least K logits reach, and as
-// the K largest logits rarely share groups (of 1024 groups' maxima the 256th is reached by some
-// 300 logits) few more do.  It is found from the first chunk of the row and again each time the
-// part of the row that has been read has doubled; in between, logits that reach the last one
-// are appended, some K more for each doubling, and what falls below the next one leaves the list.
+//   Longer rows are read once (k_top), in chunks that are each spread over the whole row.  After
+// the first chunk, and as the part read grows fourfold, the threshold is guessed: a chunk that
+// holds the part f of a row holds about K f of its K largest logits, and the logit of rank
+// K f + 4 sqrt(K f) + 4 in it lies below the row's K-th except once in a million rows (ranks are
+// taken among the maxima of groups of logits, kU groups a thread).  The vectors of logits that
+// reach the guess are noted in LDS, and at the end those that do are the list, if there are K of
+// them.  Where there are not, the K-th of the groups' maxima is a threshold that at least K logits
+// reach, and the row is read again.
 //   Where more reach it than the list holds -- many equal logits, or the largest all in a few
 // groups -- the threshold is raised by bisection over the whole row, and logits equal to the
 // last threshold are taken in the order of their indices.
@@ -43,7 +45,7 @@ struct TopShared {
     uint64_t list[kCap];
     float2 red[16];
     int redi[2][16];
-    int n;
+    int n;   // words in the list, or vectors noted
 };
 
 // Number of the workgroup's keys that reach lo; `turn` alternates between calls, which makes
@@ -63,27 +65,48 @@ __device__ __forceinline__ int count_keys(const uint32_t (&key)[J], uint32_t lo,
     return c;
 }
 
-// A threshold in [lo, hi) that at least K of the keys reach, K / 4 + 8 more at most where the
+// A threshold in [lo, hi) that at least K of the keys reach, K / 2 + 8 more at most where the
 // keys allow it; lo where fewer than K reach any other.  hi: none reaches it.  count: how many
-// reach the result (K or more only if it is not lo).
+// reach the result, if it is not lo.
 template <int NT, int J>
 __device__ uint32_t threshold(const uint32_t (&key)[J], int K, uint32_t lo, uint32_t hi, int* count,
                               TopShared& sh) {
     int turn = 0;
-    *count = 0x7fffffff;
     while (hi - lo > 1) {
         const uint32_t mid = lo + (hi - lo) / 2;
         const int c = count_keys<NT, J>(key, mid, turn++, sh);
         if (c >= K) {
             lo = mid;
             *count = c;
-            if (c <= K + K / 4 + 8) break;
+            if (c <= K + K / 2 + 8) break;
         } else {
             hi = mid;
         }
     }
     if constexpr (NT > kWave) __syncthreads();   // redi is free for the next search
     return lo;
+}
+
+// The least and the largest of the workgroup's values
+template <int NT>
+__device__ __forceinline__ void block_range(uint32_t* low, uint32_t* high, TopShared& sh) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        *low = min(*low, __shfl_xor(*low, o, kWave));
+        *high = max(*high, __shfl_xor(*high, o, kWave));
+    }
+    if constexpr (NT == kWave) return;
+    if (threadIdx.x % kWave == 0) {
+        sh.redi[0][threadIdx.x / kWave] = (int)*low;
+        sh.redi[1][threadIdx.x / kWave] = (int)*high;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NT / kWave; ++w) {
+        *low = min(*low, (uint32_t)sh.redi[0][w]);
+        *high = max(*high, (uint32_t)sh.redi[1][w]);
+    }
+    __syncthreads();
 }
 
 // The list's words each find their place among them
@@ -174,6 +197,7 @@ __global__ __launch_bounds__(NT) void k_top_short(TopArgs a) {
                 if (j * NT + tid < V) sh.list[j * NT + tid] = word_of(key[j], j * NT + tid);
             have = V;
         } else {
+            c = V;
             const uint32_t lo = threshold<NT, J>(key, K, 0, key_of(INFINITY) + 1, &c, sh);
             const uint32_t first = c > kCap ? lo + 1 : lo;   // too many equal lo
             if (tid == 0) sh.n = 0;
@@ -275,13 +299,36 @@ __device__ int select_again(const T* row, int V, int K, uint32_t lo, TopShared& 
     return c <= kCap ? have : append_equal<T, NT>(row, V, K, lo, have, sh);
 }
 
+// The threshold that K of the groups' maxima reach, at least that of key lo
+template <int NT>
+__device__ uint32_t group_threshold(const float (&group)[kU], int K, uint32_t lo, TopShared& sh) {
+    uint32_t key[kU], low = 0xffffffffu, high = 0;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+        key[u] = key_of(group[u]);
+        low = min(low, key[u]);
+        high = max(high, key[u]);
+    }
+    // the search starts between the groups' least, which all of them reach, and their largest
+    block_range<NT>(&low, &high, sh);
+    if (NT * kU >= K) lo = max(lo, low);
+    int reach = NT * kU;
+    return threshold<NT, kU>(key, K, lo, high + 1, &reach, sh);
+}
+
 template <class T, int NT>
 __global__ __launch_bounds__(NT) void k_top(TopArgs a) {
     __shared__ TopShared sh;
-    constexpr int W = kVec<T>;
-    const int tid = threadIdx.x, K = a.K, V = a.V, nv = V / W;
+    __shared__ int noted[kCap];   // vectors with a logit that reaches the threshold
+    constexpr int W = kVec<T>, kSlots = NT / kWave * kU;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const int K = a.K, V = a.V, nv = V / W;
+    // a unit is what a wave loads at once; chunk ch holds units ch, ch + chunks, ch + 2 chunks ...
+    const int units = (nv + kWave - 1) / kWave, chunks = (units + kSlots - 1) / kSlots;
     const float c = a.scale.c;
     const uint32_t rows = (uint32_t)(a.B * a.N), N = (uint32_t)a.N;
+    const uint32_t finite = key_of(-FLT_MAX);   // -inf is none of the K largest before every
+                                                // finite logit is
     for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const uint32_t b = row / N, n = row % N;
         if (n >= clamp_rows(a.lengths, b, N)) {
@@ -293,94 +340,62 @@ __global__ __launch_bounds__(NT) void k_top(TopArgs a) {
         __syncthreads();
         ChunkSoft soft;
         soft.init(c);
-        float group[kU];
+        float group[kU], least = -FLT_MAX;
 #pragma unroll
         for (int u = 0; u < kU; ++u) group[u] = -INFINITY;
-        float least = -FLT_MAX;        // the threshold: -inf is none of the K largest before
-        uint32_t lo = key_of(least);   // every finite logit is
-        bool lost = false;             // the list overflowed
-        auto append = [&](float v, int e) {
-            const int i = atomicAdd(&sh.n, 1);
-            if (i < kCap) sh.list[i] = word_of(key_of(v), e);
+        uint32_t lo = finite;   // the threshold's key
+        int next = 0;           // the chunk after which it is guessed again
+        auto note = [&](int i) {
+            const int at = atomicAdd(&sh.n, 1);
+            if (at < kCap) noted[at] = i;
         };
-        // the groups' maxima raise the threshold; what falls below it leaves the list
-        auto raise = [&](bool first) {
-            uint32_t key[kU];
-#pragma unroll
-            for (int u = 0; u < kU; ++u) key[u] = key_of(group[u]);
-            int reach;
-            lo = threshold<NT, kU>(key, K, lo, key_of(INFINITY) + 1, &reach, sh);
-            least = of_key(lo);
-            if (first) return;
-            __syncthreads();
-            const int have = sh.n;
-            lost |= have > kCap;
-            uint64_t keep[kCap / NT];
-#pragma unroll
-            for (int j = 0; j < kCap / NT; ++j) {
-                const int i = j * NT + tid;
-                keep[j] = i < have ? sh.list[i] : 0;
-            }
-            __syncthreads();
-            if (tid == 0) sh.n = 0;
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < kCap / NT; ++j)
-                if (j * NT + tid < have && (uint32_t)(keep[j] >> 32) >= lo)
-                    sh.list[atomicAdd(&sh.n, 1)] = keep[j];
-            __syncthreads();
-        };
-        const int chunks = (nv + NT * kU - 1) / (NT * kU);
-        for (int ch = 0; ch < chunks; ++ch) {
-            const int i0 = ch * NT * kU + tid;
+        auto chunk = [&](auto whole, int ch) {
+            constexpr bool kWhole = decltype(whole)::value;
+            const int i0 = (wave * kU * chunks + ch) * kWave + lane, step = chunks * kWave;
             Raw<T> r[kU];
-            float most = -INFINITY;
-            const bool whole = (ch + 1) * NT * kU <= nv;
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-                if (whole || i0 + u * NT < nv) r[u] = *(const Raw<T>*)(x + (size_t)(i0 + u * NT) * W);
             float top[kU];
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                top[u] = -INFINITY;
-                if (whole || i0 + u * NT < nv) {
-                    float v[W];
-                    unpack<T>(r[u], v);
-                    top[u] = max_of(v);
+            for (int u = 0; u < kU; ++u)
+                if (kWhole || i0 + u * step < nv)
+                    r[u] = *(const Raw<T>*)((const char*)x + (uint32_t)(i0 + u * step) * 16u);
+#pragma unroll
+            for (int h = 0; h < kU; h += 2) {
+                float v[2][W];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    top[h + u] = -INFINITY;
+                    if (kWhole || i0 + (h + u) * step < nv) {
+                        unpack<T>(r[h + u], v[u]);
+                        top[h + u] = max_of(v[u]);
+                    }
+                    group[h + u] = fmaxf(group[h + u], top[h + u]);
                 }
-                group[u] = fmaxf(group[u], top[u]);
-                most = fmaxf(most, top[u]);
+                soft.raise(fmaxf(top[h], top[h + 1]), c);
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    if (kWhole || i0 + (h + u) * step < nv) soft.push(v[u], c);
             }
-            soft.raise(most, c);
+            if (ch == next) {
+                const float part = K * (float)(ch + 1) / (float)chunks;
+                const int rank = min(K, (int)(part + 4.f * sqrtf(part) + 4.f));
+                lo = group_threshold<NT>(group, rank, lo, sh);
+                least = of_key(lo);
+                next = 4 * ch + 3;
+            }
 #pragma unroll
             for (int u = 0; u < kU; ++u)
-                if (whole || i0 + u * NT < nv) {
-                    float v[W];
-                    unpack<T>(r[u], v);
-                    soft.push(v, c);
-                }
-            if ((ch & (ch + 1)) == 0) raise(ch == 0);   // after chunks 1, 2, 4, 8 ...
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-                if ((whole || i0 + u * NT < nv) && top[u] >= least) {
-                    float v[W];
-                    unpack<T>(r[u], v);
-#pragma unroll
-                    for (int k = 0; k < W; ++k)
-                        if (v[k] >= least) append(v[k], (i0 + u * NT) * W + k);
-                }
-        }
-        const int e = nv * W + tid;   // the row's last few logits
-        if (e < V) {
-            const float v = to_f(x[e]);
-            float one[1] = {v};
-            soft.raise(v, c);
-            soft.push(one, c);
-            group[0] = fmaxf(group[0], v);
-            if (v >= least) append(v, e);
-        }
-        const float mine = fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3]));
-        raise(false);
+                if (top[u] >= least) note(i0 + u * step);
+        };
+        // all units of the last slot's chunks [0, full) are whole
+        const int full = nv / kWave - (kSlots - 1) * chunks;
+        for (int ch = 0; ch < min(full, chunks); ++ch) chunk(std::true_type{}, ch);
+        for (int ch = max(full, 0); ch < chunks; ++ch) chunk(std::false_type{}, ch);
+        const int e = nv * W + tid;   // the row's last few logits, always in the list
+        const float last = e < V ? to_f(x[e]) : -INFINITY;
+        float one[1] = {last};
+        soft.raise(last, c);
+        soft.push(one, c);
+        const float mine = fmaxf(fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3])), last);
         Soft all = block_soft<NT>(soft.value(c), c, sh.red);
         if (far(block_max<NT>(mine, (float*)sh.red))) {
             Soft again = soft_empty();
@@ -389,7 +404,30 @@ __global__ __launch_bounds__(NT) void k_top(TopArgs a) {
             all = block_soft<NT>(again, c, sh.red);
         }
         if (a.lse && tid == 0) a.lse[row] = soft_lse(all, a.scale.inv_t);
-        int have = lost ? select_again<T, NT>(x, V, K, lo, sh) : sh.n;
+        // the noted vectors' logits that reach the last threshold
+        const int vectors = sh.n;
+        __syncthreads();
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+        auto append = [&](float v, int at) {
+            const int i = atomicAdd(&sh.n, 1);
+            if (i < kCap) sh.list[i] = word_of(key_of(v), at);
+        };
+        if (last >= least) append(last, e);
+        for (int i = tid; i < min(vectors, kCap); i += NT) {
+            float v[W];
+            unpack<T>(*(const Raw<T>*)(x + (size_t)noted[i] * W), v);
+#pragma unroll
+            for (int k = 0; k < W; ++k)
+                if (v[k] >= least) append(v[k], noted[i] * W + k);
+        }
+        __syncthreads();
+        int have = sh.n;
+        __syncthreads();
+        if (vectors > kCap || have > kCap || (have < K && lo > finite)) {
+            lo = group_threshold<NT>(group, K, finite, sh);
+            have = select_again<T, NT>(x, V, K, lo, sh);
+        }
         if (have < K) have = append_equal<T, NT>(x, V, K, key_of(-INFINITY), have, sh);
         write_places<T, NT>(a, row, have, sh);
         __syncthreads();   // the list is free for the next row
