@@ -33,8 +33,6 @@ __device__ __forceinline__ float top_value(const void* p, int dtype, int64_t i) 
                                   : to_f(((const F16*)p)[i]);
 }
 
-__device__ __forceinline__ float exp_(float x) { return exp2_(x * 1.44269504f); }
-
 template <class T, int NT, bool kRest, bool kGrad>
 __global__ __launch_bounds__(NT) void k_distill(DistillArgs a) {
     extern __shared__ uint32_t marks[];   // kRest: a bit for every token

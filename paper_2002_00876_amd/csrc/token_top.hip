@@ -9,15 +9,15 @@
 // each of them finds its place there by counting the larger ones.
 //   Rows of up to 8192 logits are held in registers: the threshold is found by bisection over
 // all of them (k_top_short).
-//   Longer rows are read once (k_top), in chunks that are each spread over the whole row.  After
-// the first chunk, and as the part read grows fourfold, the threshold is guessed: a chunk that
-// holds the part f of a row holds about K f of its K largest logits, and the logit of rank
-// K f + 4 sqrt(K f) + 4 in it lies below the row's K-th except once in a million rows (ranks are
-// taken among the maxima of groups of logits, kU groups a thread).  The vectors of logits that
-// reach the guess are noted in LDS, and at the end those that do are the list, if there are K of
-// them.  Where there are not, the K-th of the groups' maxima is a threshold that at least K logits
-// reach, and the row is read again.
-//   Where more reach it than the list holds -- many equal logits, or the largest all in a few
+//   Longer rows take two launches.  k_top_scan guesses the threshold from a sample spread over the
+// row: a sample that holds the part f of a row holds about K f of its K largest logits, and the
+// logit of rank 1.5 K f + 4 sqrt(K f) + 4 in it lies below the row's K-th, unless the sample
+// happens to hold more than half again its share.  Then it reads the row once, in parts where the
+// rows are few, for the sums of its softmax, and keeps the vectors of logits that reach the guess;
+// with the threshold known its waves never wait for each other.  k_top_pick makes the list from
+// the kept vectors.  Where K logits do not reach the guess, or more vectors than are kept do, it
+// reads the row again: maxima of groups of logits give a threshold that at least K reach.
+//   Where more reach that than the list holds -- many equal logits, or the largest all in a few
 // groups -- the threshold is raised by bisection over the whole row, and logits equal to the
 // last threshold are taken in the order of their indices.
 #include <hip/hip_runtime.h>
@@ -27,8 +27,9 @@
 namespace tsc {
 namespace {
 
-constexpr int kCap = 1024;   // logits that the list holds
-constexpr int kU = 4;        // vectors of a chunk, and groups, a thread
+constexpr int kCap = 1024;    // logits that the list holds
+constexpr int kShort = 8192;  // longest rows that are held in registers
+constexpr int kTopThreads = 256;
 
 __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.0f);   // -0 + 0 = 0
@@ -52,25 +53,25 @@ struct TopShared {
 // one barrier enough
 template <int NT, int J>
 __device__ __forceinline__ int count_keys(const uint32_t (&key)[J], uint32_t lo, int turn,
-                                          TopShared& sh) {
+                                          TopShared* sh) {
     int c = 0;
 #pragma unroll
     for (int j = 0; j < J; ++j) c += __popcll(__ballot(key[j] >= lo));
     if constexpr (NT == kWave) return c;
-    if (threadIdx.x % kWave == 0) sh.redi[turn & 1][threadIdx.x / kWave] = c;
+    if (threadIdx.x % kWave == 0) sh->redi[turn & 1][threadIdx.x / kWave] = c;
     __syncthreads();
     c = 0;
 #pragma unroll
-    for (int w = 0; w < NT / kWave; ++w) c += sh.redi[turn & 1][w];
+    for (int w = 0; w < NT / kWave; ++w) c += sh->redi[turn & 1][w];
     return c;
 }
 
-// A threshold in [lo, hi) that at least K of the keys reach, K / 2 + 8 more at most where the
+// A threshold in [lo, hi) that at least K of the keys reach, K / 8 + 1 more at most where the
 // keys allow it; lo where fewer than K reach any other.  hi: none reaches it.  count: how many
 // reach the result, if it is not lo.
 template <int NT, int J>
 __device__ uint32_t threshold(const uint32_t (&key)[J], int K, uint32_t lo, uint32_t hi, int* count,
-                              TopShared& sh) {
+                              TopShared* sh = nullptr) {
     int turn = 0;
     while (hi - lo > 1) {
         const uint32_t mid = lo + (hi - lo) / 2;
@@ -78,35 +79,13 @@ __device__ uint32_t threshold(const uint32_t (&key)[J], int K, uint32_t lo, uint
         if (c >= K) {
             lo = mid;
             *count = c;
-            if (c <= K + K / 2 + 8) break;
+            if (c <= K + K / 8 + 1) break;
         } else {
             hi = mid;
         }
     }
     if constexpr (NT > kWave) __syncthreads();   // redi is free for the next search
     return lo;
-}
-
-// The least and the largest of the workgroup's values
-template <int NT>
-__device__ __forceinline__ void block_range(uint32_t* low, uint32_t* high, TopShared& sh) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        *low = min(*low, __shfl_xor(*low, o, kWave));
-        *high = max(*high, __shfl_xor(*high, o, kWave));
-    }
-    if constexpr (NT == kWave) return;
-    if (threadIdx.x % kWave == 0) {
-        sh.redi[0][threadIdx.x / kWave] = (int)*low;
-        sh.redi[1][threadIdx.x / kWave] = (int)*high;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < NT / kWave; ++w) {
-        *low = min(*low, (uint32_t)sh.redi[0][w]);
-        *high = max(*high, (uint32_t)sh.redi[1][w]);
-    }
-    __syncthreads();
 }
 
 // The list's words each find their place among them
@@ -198,7 +177,7 @@ __global__ __launch_bounds__(NT) void k_top_short(TopArgs a) {
             have = V;
         } else {
             c = V;
-            const uint32_t lo = threshold<NT, J>(key, K, 0, key_of(INFINITY) + 1, &c, sh);
+            const uint32_t lo = threshold<NT, J>(key, K, 0, key_of(INFINITY) + 1, &c, &sh);
             const uint32_t first = c > kCap ? lo + 1 : lo;   // too many equal lo
             if (tid == 0) sh.n = 0;
             __syncthreads();
@@ -230,7 +209,7 @@ __device__ void collect(const T* row, int V, uint32_t lo, TopShared& sh) {
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
     const float least = of_key(lo);
-    walk_row<T, NT, 4>(row, 0, V, threadIdx.x, [&](const float (&v)[kVec<T>], int at, int num) {
+    walk_row<T, NT, 1>(row, 0, V, threadIdx.x, [&](const float (&v)[kVec<T>], int at, int num) {
 #pragma unroll
         for (int k = 0; k < kVec<T>; ++k)
             if (k < num && v[k] >= least) {
@@ -245,7 +224,7 @@ template <class T, int NT>
 __device__ int count_row(const T* row, int V, uint32_t lo, TopShared& sh) {
     int c = 0;
     const float least = of_key(lo);
-    walk_row<T, NT, 4>(row, 0, V, threadIdx.x, [&](const float (&v)[kVec<T>], int, int num) {
+    walk_row<T, NT, 1>(row, 0, V, threadIdx.x, [&](const float (&v)[kVec<T>], int, int num) {
 #pragma unroll
         for (int k = 0; k < kVec<T>; ++k) c += k < num && v[k] >= least;
     });
@@ -299,146 +278,322 @@ __device__ int select_again(const T* row, int V, int K, uint32_t lo, TopShared& 
     return c <= kCap ? have : append_equal<T, NT>(row, V, K, lo, have, sh);
 }
 
-// The threshold that K of the groups' maxima reach, at least that of key lo
-template <int NT>
-__device__ uint32_t group_threshold(const float (&group)[kU], int K, uint32_t lo, TopShared& sh) {
-    uint32_t key[kU], low = 0xffffffffu, high = 0;
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-        key[u] = key_of(group[u]);
-        low = min(low, key[u]);
-        high = max(high, key[u]);
-    }
-    // the search starts between the groups' least, which all of them reach, and their largest
-    block_range<NT>(&low, &high, sh);
-    if (NT * kU >= K) lo = max(lo, low);
-    int reach = NT * kU;
-    return threshold<NT, kU>(key, K, lo, high + 1, &reach, sh);
+constexpr int kScanThreads = 256;
+constexpr int kSample = 4;        // vectors a thread in the sample
+constexpr int kKeep = 252;        // vectors that a wave keeps: 8 workgroups fill a CU's LDS
+constexpr int kScanWaves = kScanThreads / kWave;
+constexpr int kScanWant = 2048;   // workgroups that fill the chip
+constexpr int kMinScan = 2048;    // elements of a part
+constexpr int64_t kSlab = 4096;   // parts of rows that the workspace holds at once
+
+struct TopPlan {
+    int parts;
+    int64_t rows;     // of a slab
+    float* least;     // [rows]
+    float4* sums;     // [rows][parts]: maximum and sum of the softmax, largest logit
+    int32_t* count;   // [rows][parts][kScanWaves]: vectors that reach the threshold
+    int32_t* at;      // [rows][parts][kScanWaves][kKeep]: their numbers
+    Vec4* kept;       // [rows][parts][kScanWaves][kKeep]: and what they hold
+    size_t bytes;
+};
+TopPlan top_plan(int64_t rows, int64_t V, void* ws) {
+    TopPlan p;
+    int64_t parts = (kScanWant + rows - 1) / rows;
+    const int64_t most = (V + kMinScan - 1) / kMinScan;
+    if (parts > most) parts = most;
+    if (parts > kWave) parts = kWave;
+    p.parts = parts < 1 ? 1 : (int)parts;
+    p.rows = rows < kSlab / p.parts ? rows : kSlab / p.parts;
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        char* at = (char*)ws + off;
+        off += (bytes + 255) / 256 * 256;
+        return at;
+    };
+    const size_t n = (size_t)p.rows * p.parts;
+    p.least = (float*)take((size_t)p.rows * sizeof(float));
+    p.sums = (float4*)take(n * sizeof(float4));
+    p.count = (int32_t*)take(n * kScanWaves * sizeof(int32_t));
+    p.at = (int32_t*)take(n * kScanWaves * kKeep * sizeof(int32_t));
+    p.kept = (Vec4*)take(n * kScanWaves * kKeep * sizeof(Vec4));
+    p.bytes = off;
+    return p;
 }
 
-template <class T, int NT>
-__global__ __launch_bounds__(NT) void k_top(TopArgs a) {
-    __shared__ TopShared sh;
-    __shared__ int noted[kCap];   // vectors with a logit that reaches the threshold
-    constexpr int W = kVec<T>, kSlots = NT / kWave * kU;
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    const int K = a.K, V = a.V, nv = V / W;
-    // a unit is what a wave loads at once; chunk ch holds units ch, ch + chunks, ch + 2 chunks ...
-    const int units = (nv + kWave - 1) / kWave, chunks = (units + kSlots - 1) / kSlots;
-    const float c = a.scale.c;
-    const uint32_t rows = (uint32_t)(a.B * a.N), N = (uint32_t)a.N;
-    const uint32_t finite = key_of(-FLT_MAX);   // -inf is none of the K largest before every
-                                                // finite logit is
-    for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        const uint32_t b = row / N, n = row % N;
-        if (n >= clamp_rows(a.lengths, b, N)) {
-            write_padding<T, NT>(a, row);
-            continue;
-        }
-        const T* x = row_of<T>(a.logits, b, n);
-        if (tid == 0) sh.n = 0;
-        __syncthreads();
-        ChunkSoft soft;
-        soft.init(c);
-        float group[kU], least = -FLT_MAX;
+struct ScanShared {
+    union {
+        uint32_t key[kScanThreads * kSample];   // the sample's
+        Vec4 kept[kScanWaves][kKeep];
+    };
+    int at[kScanWaves][kKeep];
+    float2 red[kScanWaves];
+    float least;
+};
+
+// The threshold guessed from the largest logits of a sample's vectors, by one wave
+__device__ uint32_t guess(const uint32_t* keys, int K, float sampled) {
+    constexpr int J = kScanThreads * kSample / kWave;
+    uint32_t key[J], high = 0;
 #pragma unroll
-        for (int u = 0; u < kU; ++u) group[u] = -INFINITY;
-        uint32_t lo = finite;   // the threshold's key
-        int next = 0;           // the chunk after which it is guessed again
-        auto note = [&](int i) {
-            const int at = atomicAdd(&sh.n, 1);
-            if (at < kCap) noted[at] = i;
-        };
-        auto chunk = [&](auto whole, int ch) {
-            constexpr bool kWhole = decltype(whole)::value;
-            const int i0 = (wave * kU * chunks + ch) * kWave + lane, step = chunks * kWave;
-            Raw<T> r[kU];
-            float top[kU];
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-                if (kWhole || i0 + u * step < nv)
-                    r[u] = *(const Raw<T>*)((const char*)x + (uint32_t)(i0 + u * step) * 16u);
-#pragma unroll
-            for (int h = 0; h < kU; h += 2) {
-                float v[2][W];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    top[h + u] = -INFINITY;
-                    if (kWhole || i0 + (h + u) * step < nv) {
-                        unpack<T>(r[h + u], v[u]);
-                        top[h + u] = max_of(v[u]);
-                    }
-                    group[h + u] = fmaxf(group[h + u], top[h + u]);
-                }
-                soft.raise(fmaxf(top[h], top[h + 1]), c);
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    if (kWhole || i0 + (h + u) * step < nv) soft.push(v[u], c);
-            }
-            if (ch == next) {
-                const float part = K * (float)(ch + 1) / (float)chunks;
-                const int rank = min(K, (int)(part + 4.f * sqrtf(part) + 4.f));
-                lo = group_threshold<NT>(group, rank, lo, sh);
-                least = of_key(lo);
-                next = 4 * ch + 3;
-            }
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-                if (top[u] >= least) note(i0 + u * step);
-        };
-        // all units of the last slot's chunks [0, full) are whole
-        const int full = nv / kWave - (kSlots - 1) * chunks;
-        for (int ch = 0; ch < min(full, chunks); ++ch) chunk(std::true_type{}, ch);
-        for (int ch = max(full, 0); ch < chunks; ++ch) chunk(std::false_type{}, ch);
-        const int e = nv * W + tid;   // the row's last few logits, always in the list
-        const float last = e < V ? to_f(x[e]) : -INFINITY;
-        float one[1] = {last};
-        soft.raise(last, c);
-        soft.push(one, c);
-        const float mine = fmaxf(fmaxf(fmaxf(group[0], group[1]), fmaxf(group[2], group[3])), last);
-        Soft all = block_soft<NT>(soft.value(c), c, sh.red);
-        if (far(block_max<NT>(mine, (float*)sh.red))) {
-            Soft again = soft_empty();
-            walk_row<T, NT, 4>(x, 0, V, tid,
-                               [&](const float (&v)[W], int, int) { soft_push(again, v, c); });
-            all = block_soft<NT>(again, c, sh.red);
-        }
-        if (a.lse && tid == 0) a.lse[row] = soft_lse(all, a.scale.inv_t);
-        // the noted vectors' logits that reach the last threshold
-        const int vectors = sh.n;
-        __syncthreads();
-        if (tid == 0) sh.n = 0;
-        __syncthreads();
-        auto append = [&](float v, int at) {
-            const int i = atomicAdd(&sh.n, 1);
-            if (i < kCap) sh.list[i] = word_of(key_of(v), at);
-        };
-        if (last >= least) append(last, e);
-        for (int i = tid; i < min(vectors, kCap); i += NT) {
-            float v[W];
-            unpack<T>(*(const Raw<T>*)(x + (size_t)noted[i] * W), v);
-#pragma unroll
-            for (int k = 0; k < W; ++k)
-                if (v[k] >= least) append(v[k], noted[i] * W + k);
-        }
-        __syncthreads();
-        int have = sh.n;
-        __syncthreads();
-        if (vectors > kCap || have > kCap || (have < K && lo > finite)) {
-            lo = group_threshold<NT>(group, K, finite, sh);
-            have = select_again<T, NT>(x, V, K, lo, sh);
-        }
-        if (have < K) have = append_equal<T, NT>(x, V, K, key_of(-INFINITY), have, sh);
-        write_places<T, NT>(a, row, have, sh);
-        __syncthreads();   // the list is free for the next row
+    for (int j = 0; j < J; ++j) {
+        key[j] = keys[j * kWave + threadIdx.x];
+        high = max(high, key[j]);
     }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) high = max(high, __shfl_xor(high, o, kWave));
+    const float part = K * fminf(sampled, 1.f);
+    const float rank = fminf(K * 1.25f + 8.f, 1.5f * part + 4.f * sqrtf(part) + 4.f);
+    // `rank` logits lie in about this many different ones of so many groups
+    auto reach = [&](float groups) { return max(1, (int)(groups * (1.f - exp_(-rank / groups)))); };
+    const uint32_t low = key_of(-FLT_MAX), top = __builtin_amdgcn_readfirstlane(high) + 1;
+    int c;
+    if (rank > 100.f) return threshold<kWave, J>(key, reach(J * kWave), low, top, &c);
+    // (a step of the search takes the time of its keys)
+    uint32_t of4[J / 4];
+#pragma unroll
+    for (int j = 0; j < J / 4; ++j)
+        of4[j] = max(max(key[j], key[j + J / 4]), max(key[j + J / 2], key[j + J / 4 * 3]));
+    return threshold<kWave, J / 4>(of4, reach(J / 4 * kWave), low, top, &c);
+}
+
+// One workgroup a part of a row: sums of its softmax, and the vectors that reach the threshold.
+// They are kept in LDS until the end: the loads' waits would count their stores to memory.
+template <class T>
+__global__ __launch_bounds__(kScanThreads, 8) void k_top_scan(TopArgs a, TopPlan p, uint32_t first,
+                                                              uint32_t rows) {
+    __shared__ ScanShared sh;
+    constexpr int NT = kScanThreads, W = kVec<T>;
+    const uint32_t i = blockIdx.x / (uint32_t)p.parts, part = blockIdx.x % (uint32_t)p.parts;
+    if (i >= rows) return;
+    const uint32_t row = first + i, b = row / (uint32_t)a.N, n = row % (uint32_t)a.N;
+    if (n >= clamp_rows(a.lengths, b, a.N)) return;
+    const T* x = row_of<T>(a.logits, b, n);
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, nv = a.V / W;
+    {
+        // a 16th of the row at least, an 8th where the list would be long: units of 64 vectors
+        constexpr int kRound = kScanWaves * kSample, kOnce = NT * kSample * W;
+        const int units = (nv + kWave - 1) / kWave;
+        const int rounds = (a.V * (a.K > 128 ? 2 : 1) + 16 * kOnce - 1) / (16 * kOnce);
+        float top[kSample];
+        for (int q = 0; q < rounds; ++q) {
+            Raw<T> r[kSample];
+#pragma unroll
+            for (int j = 0; j < kSample; ++j) {
+                const int u = ((wave * kSample + j) * rounds + q) * units / (kRound * rounds);
+                r[j] = load_raw<T, false>(x + (size_t)min(u * kWave + lane, nv - 1) * W);
+            }
+#pragma unroll
+            for (int j = 0; j < kSample; ++j) {
+                float v[W];
+                unpack<T>(r[j], v);
+                top[j] = q ? fmaxf(top[j], max_of(v)) : max_of(v);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kSample; ++j) sh.key[j * NT + tid] = key_of(top[j]);
+        __syncthreads();
+        if (tid < kWave) {
+            const uint32_t lo = guess(sh.key, a.K, (float)(rounds * kOnce) / (float)a.V);
+            if (tid == 0) {
+                sh.least = of_key(lo);
+                if (part == 0) p.least[i] = sh.least;
+            }
+        }
+        __syncthreads();
+    }
+    const int per = ((nv + p.parts - 1) / p.parts + 7) / 8 * 8;   // whole cache lines
+    const int lo = min((int)part * per, nv), hi = min(lo + per, nv);
+    const float c = a.scale.c, least = sh.least;
+    ChunkSoft soft;
+    soft.init(c);
+    float most = -INFINITY;
+    int found = 0;   // of this wave
+    auto keep = [&](bool reaches, const Raw<T>& r, int v) {
+        const uint64_t votes = __ballot(reaches);
+        const int k = found + __builtin_amdgcn_mbcnt_hi((uint32_t)(votes >> 32),
+                                                        __builtin_amdgcn_mbcnt_lo((uint32_t)votes, 0));
+        if (reaches && k < kKeep) {
+            sh.kept[wave][k] = {r.w[0], r.w[1], r.w[2], r.w[3]};
+            sh.at[wave][k] = v;
+        }
+        found += __popcll(votes);
+    };
+    auto work = [&](const Raw<T> (&r)[2], int v0, int v1) {
+        float v[2][W], top[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            unpack<T>(r[u], v[u]);
+            top[u] = max_of(v[u]);
+        }
+        const float t = fmaxf(top[0], top[1]);
+        most = fmaxf(most, t);
+        soft.raise(t, c);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) soft.push(v[u], c);
+        if (__any(t >= least)) {
+            keep(top[0] >= least, r[0], v0);
+            keep(top[1] >= least, r[1], v1);
+        }
+    };
+    const char* base = (const char*)x;
+    auto load = [&](int v) { return load_raw<T, true>((const T*)(base + (uint32_t)v * 16u)); };
+    int v = lo + tid;
+    for (; v + 3 * NT < hi; v += 4 * NT) {
+        Raw<T> r[2], s[2];
+        r[0] = load(v), r[1] = load(v + NT), s[0] = load(v + 2 * NT), s[1] = load(v + 3 * NT);
+        work(r, v, v + NT);
+        work(s, v + 2 * NT, v + 3 * NT);
+    }
+    // a wave's first lane is in every turn that any of its lanes is in, and has counted them all
+    found = __builtin_amdgcn_readfirstlane(found);
+    for (; v < hi; v += NT) {
+        Raw<T> r[2] = {load(v), {}};
+        float one[W];
+        unpack<T>(r[0], one);
+        const float t = max_of(one);
+        most = fmaxf(most, t);
+        soft.raise(t, c);
+        soft.push(one, c);
+        keep(t >= least, r[0], v);
+    }
+    found = __builtin_amdgcn_readfirstlane(found);
+    const int e = nv * W + tid;   // the row's last few logits; k_top_pick looks at all of them
+    if (part == 0 && e < a.V) {
+        float one[1] = {to_f(x[e])};
+        most = fmaxf(most, one[0]);
+        soft.raise(one[0], c);
+        soft.push(one, c);
+    }
+    const Soft all = block_soft<NT>(soft.value(c), c, sh.red);
+    most = block_max<NT>(most, (float*)sh.red);
+    if (tid == 0) {
+        p.sums[blockIdx.x] = make_float4(all.m, all.s, most, 0.f);
+    }
+    const size_t q = (size_t)blockIdx.x * kScanWaves + wave;
+    if (lane == 0) p.count[q] = found;
+    for (int k = lane; k < min(found, kKeep); k += kWave) {
+        p.kept[q * kKeep + k] = sh.kept[wave][k];
+        p.at[q * kKeep + k] = sh.at[wave][k];
+    }
+}
+
+// A threshold that at least K of the row's logits reach, from the maxima of groups of them
+template <class T, int NT>
+__device__ uint32_t group_threshold(const T* row, int V, int K, TopShared& sh) {
+    constexpr int kU = 4;
+    float group[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) group[u] = -INFINITY;
+    int turn = 0;
+    walk_row<T, NT, 1>(row, 0, V, threadIdx.x, [&](const float (&v)[kVec<T>], int, int) {
+        const float t = max_of(v);
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+            if ((turn & (kU - 1)) == u) group[u] = fmaxf(group[u], t);
+        ++turn;
+    });
+    uint32_t key[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) key[u] = key_of(group[u]);
+    int c;
+    return threshold<NT, kU>(key, K, key_of(-FLT_MAX), key_of(INFINITY) + 1, &c, &sh);
+}
+
+// One workgroup a row: the list from the kept vectors
+template <class T>
+__global__ __launch_bounds__(kTopThreads) void k_top_pick(TopArgs a, TopPlan p, uint32_t first,
+                                                          uint32_t rows) {
+    __shared__ TopShared sh;
+    constexpr int NT = kTopThreads, W = kVec<T>, J = kCap / NT;
+    const int tid = threadIdx.x, K = a.K, V = a.V;
+    const uint32_t i = blockIdx.x;
+    if (i >= rows) return;
+    const uint32_t row = first + i, b = row / (uint32_t)a.N, n = row % (uint32_t)a.N;
+    if (n >= clamp_rows(a.lengths, b, a.N)) {
+        write_padding<T, NT>(a, row);
+        return;
+    }
+    const T* x = row_of<T>(a.logits, b, n);
+    const float c = a.scale.c, least = p.least[i];
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    auto append = [&](float v, int at) {
+        const int k = atomicAdd(&sh.n, 1);
+        if (k < kCap) sh.list[k] = word_of(key_of(v), at);
+    };
+    bool lost = false;
+    Soft soft = soft_empty();
+    float most = -INFINITY;
+    for (int part = 0; part < p.parts; ++part) {
+        const float4 s = p.sums[(size_t)i * p.parts + part];
+        soft = soft_merge(soft, {s.x, s.y}, c);
+        most = fmaxf(most, s.z);
+    }
+    // a wave for each of the scan's
+    static_assert(NT / kWave == kScanWaves);
+    for (int part = 0; part < p.parts; ++part) {
+        const size_t q = ((size_t)i * p.parts + part) * kScanWaves + tid / kWave;
+        const int count = p.count[q];
+        lost |= count > kKeep;
+        for (int k = tid % kWave; k < min(count, kKeep); k += kWave) {
+            const Vec4 w = p.kept[q * kKeep + k];
+            const int at = p.at[q * kKeep + k] * W;
+            float v[W];
+            unpack<T>({{w.x, w.y, w.z, w.w}}, v);
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                if (v[e] >= least) append(v[e], at + e);
+        }
+    }
+    const int e = V / W * W + tid;   // the row's last few logits
+    if (e < V && to_f(x[e]) >= least) append(to_f(x[e]), e);
+    if (a.lse) {
+        if (far(most)) {
+            soft = soft_empty();
+            walk_row<T, NT, 1>(x, 0, V, tid,
+                               [&](const float (&v)[W], int, int) { soft_push(soft, v, c); });
+            soft = block_soft<NT>(soft, c, sh.red);
+        }
+        if (tid == 0) a.lse[row] = soft_lse(soft, a.scale.inv_t);
+    }
+    lost = __syncthreads_or(lost);
+    int have = sh.n;
+    __syncthreads();
+    if (lost || have > kCap || (have < K && least > -FLT_MAX)) {
+        have = select_again<T, NT>(x, V, K, group_threshold<T, NT>(x, V, K, sh), sh);
+    } else if (have > K + K / 4 + 32) {
+        // counting takes the square of the list's length: what the K-th is above leaves it
+        uint64_t w[J];
+        uint32_t key[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            w[j] = j * NT + tid < have ? sh.list[j * NT + tid] : 0;
+            key[j] = (uint32_t)(w[j] >> 32);
+        }
+        int reach;
+        const uint32_t lo = threshold<NT, J>(key, K, key_of(least), key_of(INFINITY) + 1, &reach, &sh);
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (key[j] >= lo) sh.list[atomicAdd(&sh.n, 1)] = w[j];
+        __syncthreads();
+        have = sh.n;
+    }
+    // -inf is none of the K largest before every finite logit is
+    if (have < K) have = append_equal<T, NT>(x, V, K, key_of(-INFINITY), have, sh);
+    __syncthreads();
+    write_places<T, NT>(a, row, have, sh);
 }
 
 }  // namespace
 
-size_t top_workspace(int64_t, int64_t, int64_t, int64_t) { return 0; }
+size_t top_workspace(int64_t B, int64_t N, int64_t V, int64_t) {
+    return V <= kShort ? 0 : top_plan(B * N, V, nullptr).bytes;
+}
 
 hipError_t launch_top(const TopArgs& a, hipStream_t s) {
+    hipError_t e = hipSuccess;
     with_type(a.dtype, [&](auto t) {
         using T = decltype(t);
         const int64_t rows = a.B * a.N;
@@ -451,12 +606,20 @@ hipError_t launch_top(const TopArgs& a, hipStream_t s) {
             k_top_short<T, 64, 16><<<g1, 64, 0, s>>>(a);
         else if (a.V <= 4096)
             k_top_short<T, 256, 16><<<g4, 256, 0, s>>>(a);
-        else if (a.V <= 8192)
+        else if (a.V <= kShort)
             k_top_short<T, 256, 32><<<g4, 256, 0, s>>>(a);
-        else
-            k_top<T, 256><<<g4, 256, 0, s>>>(a);
+        else {
+            const TopPlan p = top_plan(rows, a.V, a.ws);
+            for (int64_t first = 0; first < rows && e == hipSuccess; first += p.rows) {
+                const uint32_t n = (uint32_t)(rows - first < p.rows ? rows - first : p.rows);
+                const uint32_t at = (uint32_t)first;
+                k_top_scan<T><<<n * p.parts, kScanThreads, 0, s>>>(a, p, at, n);
+                k_top_pick<T><<<n, kTopThreads, 0, s>>>(a, p, at, n);
+                e = hipGetLastError();
+            }
+        }
     });
-    return hipGetLastError();
+    return e == hipSuccess ? hipGetLastError() : e;
 }
 
 }  // namespace tsc
