@@ -7,8 +7,8 @@
 //
 // A threshold that K logits reach is found, the logits that reach it go into a list in LDS, and
 // each of them finds its place there by counting the larger ones.
-//   Rows of up to 8192 logits are held in registers: the threshold is found by bisection over
-// all of them (k_top_short).
+//   Rows of up to 1024 logits are held in a wave's registers: the threshold is found by bisection
+// (k_top_short).
 //   Longer rows take two launches.  k_top_scan guesses the threshold from a sample spread over the
 // row: a sample that holds the part f of a row holds about K f of its K largest logits, and the
 // logit of rank 1.5 K f + 4 sqrt(K f) + 4 in it lies below the row's K-th, unless the sample
@@ -28,7 +28,7 @@ namespace tsc {
 namespace {
 
 constexpr int kCap = 1024;    // logits that the list holds
-constexpr int kShort = 8192;  // longest rows that are held in registers
+constexpr int kShort = 1024;  // longest rows that a wave holds in its registers
 constexpr int kTopThreads = 256;
 
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -42,12 +42,14 @@ __device__ __forceinline__ uint64_t word_of(uint32_t key, int index) {
     return (uint64_t)key << 32 | (uint32_t)~index;
 }
 
-struct TopShared {
-    uint64_t list[kCap];
+template <int kWords>
+struct TopSharedOf {
+    uint64_t list[kWords];
     float2 red[16];
     int redi[2][16];
     int n;   // words in the list, or vectors noted
 };
+using TopShared = TopSharedOf<kCap>;
 
 // Number of the workgroup's keys that reach lo; `turn` alternates between calls, which makes
 // one barrier enough
@@ -89,9 +91,8 @@ __device__ uint32_t threshold(const uint32_t (&key)[J], int K, uint32_t lo, uint
 }
 
 // The list's words each find their place among them
-template <class T, int NT>
-__device__ __forceinline__ void write_places(const TopArgs& a, uint32_t row, int n,
-                                             const TopShared& sh) {
+template <class T, int NT, class S>
+__device__ __forceinline__ void write_places(const TopArgs& a, uint32_t row, int n, const S& sh) {
     T* values = (T*)a.values + (size_t)row * a.K;
     int32_t* indices = a.indices + (size_t)row * a.K;
     for (int i = threadIdx.x; i < n; i += NT) {
@@ -118,9 +119,8 @@ __device__ __forceinline__ void write_padding(const TopArgs& a, uint32_t row) {
 }
 
 // Puts the threads' hits into the list in the order of (call, thread); have: the words in it
-template <int NT>
-__device__ __forceinline__ int append_ordered(bool hit, uint64_t word, int have, int most,
-                                              TopShared& sh) {
+template <int NT, class S>
+__device__ __forceinline__ int append_ordered(bool hit, uint64_t word, int have, int most, S& sh) {
     const uint64_t votes = __ballot(hit);
     int before = 0, all = __popcll(votes);
     if constexpr (NT > kWave) {
@@ -139,10 +139,11 @@ __device__ __forceinline__ int append_ordered(bool hit, uint64_t word, int have,
     return min(have + all, most);
 }
 
-// Rows of up to NT * J logits
-template <class T, int NT, int J>
-__global__ __launch_bounds__(NT) void k_top_short(TopArgs a) {
-    __shared__ TopShared sh;
+// Rows of up to 64 * J logits, a wave each
+template <class T, int J>
+__global__ __launch_bounds__(kWave) void k_top_short(TopArgs a) {
+    constexpr int NT = kWave;
+    __shared__ TopSharedOf<kWave * J> sh;
     const int tid = threadIdx.x, K = a.K, V = a.V;
     const uint32_t rows = (uint32_t)(a.B * a.N), N = (uint32_t)a.N;
     for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x) {
@@ -159,41 +160,43 @@ __global__ __launch_bounds__(NT) void k_top_short(TopArgs a) {
             v[j] = e < V ? to_f(x[e]) : -INFINITY;
         }
         Soft soft = soft_empty();
-        uint32_t key[J];
+        uint32_t key[J], mine = 0;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             soft.m = fmaxf(soft.m, v[j]);
             key[j] = j * NT + tid < V ? key_of(v[j]) : 0u;   // 0: below every logit's
+            mine = max(mine, key[j]);
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) soft.s += exp2_((v[j] - soft.m) * a.scale.c);
         soft = block_soft<NT>(soft, a.scale.c, sh.red);
         if (a.lse && tid == 0) a.lse[row] = soft_lse(soft, a.scale.inv_t);
-        int have = 0, c;
-        if (V <= kCap && V <= 2 * K + 64) {   // a search would leave out little
-#pragma unroll
-            for (int j = 0; j < J; ++j)
-                if (j * NT + tid < V) sh.list[j * NT + tid] = word_of(key[j], j * NT + tid);
-            have = V;
-        } else {
-            c = V;
-            const uint32_t lo = threshold<NT, J>(key, K, 0, key_of(INFINITY) + 1, &c, &sh);
-            const uint32_t first = c > kCap ? lo + 1 : lo;   // too many equal lo
-            if (tid == 0) sh.n = 0;
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < J; ++j)
-                if (key[j] >= first) sh.list[atomicAdd(&sh.n, 1)] = word_of(key[j], j * NT + tid);
-            __syncthreads();
-            have = sh.n;
-            if (c > kCap)
-                for (int j = 0; j < J && have < K; ++j) {
-                    uint32_t kj = key[0];
-#pragma unroll
-                    for (int i = 1; i < J; ++i) kj = i == j ? key[i] : kj;
-                    have = append_ordered<NT>(kj == lo, word_of(lo, j * NT + tid), have, K, sh);
-                }
+        const int enough = 2 * K + 64;   // words that are soon counted
+        uint32_t lo = 1;                 // every logit's key reaches it
+        int c = V;
+        if (V > enough) {
+            // lanes' largest logits first: what K of them reach, K logits reach
+            const uint32_t hi = key_of(INFINITY) + 1;
+            const uint32_t one[1] = {mine};
+            if (K <= kWave / 2) lo = threshold<NT, 1>(one, K, lo, hi, &c);
+            c = count_keys<NT, J>(key, lo, 0, nullptr);
+            if (c > enough) lo = threshold<NT, J>(key, K, lo, hi, &c);
         }
+        // too many that equal lo: those above it, and the first of these
+        const uint32_t first = c > enough ? lo + 1 : lo;
+        int have = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (j * NT < V)
+                have = append_ordered<NT>(key[j] >= first, word_of(key[j], j * NT + tid), have,
+                                          kWave * J, sh);
+        if (c > enough)
+            for (int j = 0; j < J && have < K; ++j) {
+                uint32_t kj = key[0];
+#pragma unroll
+                for (int i = 1; i < J; ++i) kj = i == j ? key[i] : kj;
+                have = append_ordered<NT>(kj == lo, word_of(lo, j * NT + tid), have, K, sh);
+            }
         __syncthreads();
         write_places<T, NT>(a, row, have, sh);
         __syncthreads();   // the list is free for the next row
@@ -301,7 +304,7 @@ TopPlan top_plan(int64_t rows, int64_t V, void* ws) {
     int64_t parts = (kScanWant + rows - 1) / rows;
     const int64_t most = (V + kMinScan - 1) / kMinScan;
     if (parts > most) parts = most;
-    if (parts > kWave) parts = kWave;
+    if (parts > kTopThreads / kScanWaves) parts = kTopThreads / kScanWaves;
     p.parts = parts < 1 ? 1 : (int)parts;
     p.rows = rows < kSlab / p.parts ? rows : kSlab / p.parts;
     size_t off = 0;
@@ -377,16 +380,21 @@ __global__ __launch_bounds__(kScanThreads, 8) void k_top_scan(TopArgs a, TopPlan
         float top[kSample];
         for (int q = 0; q < rounds; ++q) {
             Raw<T> r[kSample];
+            bool there[kSample];
 #pragma unroll
             for (int j = 0; j < kSample; ++j) {
-                const int u = ((wave * kSample + j) * rounds + q) * units / (kRound * rounds);
+                // (rows of no more units than the sample has are taken whole)
+                const int at = (wave * kSample + j) * rounds + q;
+                const int u = units <= kRound ? at : at * units / (kRound * rounds);
                 r[j] = load_raw<T, false>(x + (size_t)min(u * kWave + lane, nv - 1) * W);
+                there[j] = u * kWave + lane < nv;
             }
 #pragma unroll
             for (int j = 0; j < kSample; ++j) {
                 float v[W];
                 unpack<T>(r[j], v);
-                top[j] = q ? fmaxf(top[j], max_of(v)) : max_of(v);
+                const float t = there[j] ? max_of(v) : -INFINITY;
+                top[j] = q ? fmaxf(top[j], t) : t;
             }
         }
 #pragma unroll
@@ -523,19 +531,21 @@ __global__ __launch_bounds__(kTopThreads) void k_top_pick(TopArgs a, TopPlan p, 
     };
     bool lost = false;
     Soft soft = soft_empty();
-    float most = -INFINITY;
-    for (int part = 0; part < p.parts; ++part) {
-        const float4 s = p.sums[(size_t)i * p.parts + part];
-        soft = soft_merge(soft, {s.x, s.y}, c);
-        most = fmaxf(most, s.z);
+    float most;
+    {
+        const int lane = tid % kWave;
+        const float4 s = lane < p.parts ? p.sums[(size_t)i * p.parts + lane]
+                                        : make_float4(-FLT_MAX, 0.f, -INFINITY, 0.f);
+        soft = wave_soft({s.x, s.y}, c);
+        most = wave_max_fast(s.z);
     }
-    // a wave for each of the scan's
-    static_assert(NT / kWave == kScanWaves);
-    for (int part = 0; part < p.parts; ++part) {
-        const size_t q = ((size_t)i * p.parts + part) * kScanWaves + tid / kWave;
+    // the scan's waves' vectors, `each` threads to a wave's
+    const int lists = p.parts * kScanWaves, each = NT / lists;
+    if (tid < lists * each) {
+        const size_t q = (size_t)i * lists + tid / each;
         const int count = p.count[q];
-        lost |= count > kKeep;
-        for (int k = tid % kWave; k < min(count, kKeep); k += kWave) {
+        lost = count > kKeep;
+        for (int k = tid % each; k < min(count, kKeep); k += each) {
             const Vec4 w = p.kept[q * kKeep + k];
             const int at = p.at[q * kKeep + k] * W;
             float v[W];
@@ -597,17 +607,13 @@ hipError_t launch_top(const TopArgs& a, hipStream_t s) {
     with_type(a.dtype, [&](auto t) {
         using T = decltype(t);
         const int64_t rows = a.B * a.N;
-        const unsigned g1 = row_grid(rows, 64), g4 = row_grid(rows, 256);
+        const unsigned grid = row_grid(rows, kWave);
         if (a.V <= 64)
-            k_top_short<T, 64, 1><<<g1, 64, 0, s>>>(a);
+            k_top_short<T, 1><<<grid, kWave, 0, s>>>(a);
         else if (a.V <= 256)
-            k_top_short<T, 64, 4><<<g1, 64, 0, s>>>(a);
-        else if (a.V <= 1024)
-            k_top_short<T, 64, 16><<<g1, 64, 0, s>>>(a);
-        else if (a.V <= 4096)
-            k_top_short<T, 256, 16><<<g4, 256, 0, s>>>(a);
+            k_top_short<T, 4><<<grid, kWave, 0, s>>>(a);
         else if (a.V <= kShort)
-            k_top_short<T, 256, 32><<<g4, 256, 0, s>>>(a);
+            k_top_short<T, 16><<<grid, kWave, 0, s>>>(a);
         else {
             const TopPlan p = top_plan(rows, a.V, a.ws);
             for (int64_t first = 0; first < rows && e == hipSuccess; first += p.rows) {
