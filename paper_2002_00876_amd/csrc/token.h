@@ -55,6 +55,13 @@ __device__ __forceinline__ Raw<T> load_raw(const T* at) {
     return {{v.x, v.y, v.z, v.w}};
 }
 
+// Stores a vector that nothing will read soon
+template <class T>
+__device__ __forceinline__ void store_raw(T* at, const Raw<T>& r) {
+    using Vec = std::conditional_t<sizeof(T) == 4, Vec4, Vec2>;
+    __builtin_nontemporal_store(Vec{r.w[0], r.w[1], r.w[2], r.w[3]}, (Vec*)at);
+}
+
 __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(Bf16 x) { return __uint_as_float((uint32_t)x.u << 16); }
 __device__ __forceinline__ float to_f(F16 x) { return (float)__builtin_bit_cast(_Float16, x.u); }
@@ -137,7 +144,8 @@ __device__ __forceinline__ void walk_row(const T* row, int lo, int hi, int tid, 
     }
 }
 
-// Running maximum and sum of numerators.  The empty state's maximum is the lowest float, not
+// Running maximum and sum of numerators.  Sums are not contracted, so that kernels which share these
+// give the same bits, however each of them is compiled.  The empty state's maximum is the lowest float, not
 // -inf, so that differences to it are never NaN.
 struct Soft {
     float m, s;
@@ -147,6 +155,7 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 __device__ __forceinline__ float exp_(float x) { return exp2_(x * 1.44269504f); }
 template <int W>
 __device__ __forceinline__ void soft_push(Soft& a, const float (&v)[W], float c) {
+#pragma clang fp contract(off)
     float m = a.m;
 #pragma unroll
     for (int k = 0; k < W; ++k) m = fmaxf(m, v[k]);
@@ -156,52 +165,50 @@ __device__ __forceinline__ void soft_push(Soft& a, const float (&v)[W], float c)
     a = {m, s};
 }
 __device__ __forceinline__ Soft soft_merge(Soft a, Soft b, float c) {
+#pragma clang fp contract(off)
     const float m = fmaxf(a.m, b.m);
     return {m, a.s * exp2_((a.m - m) * c) + b.s * exp2_((b.m - m) * c)};
 }
 __device__ __forceinline__ Soft wave_soft(Soft a, float c) {
+#pragma clang fp contract(off)
     const float m = wave_max_fast(a.m);
     return {m, wave_sum_fast(a.s * exp2_((a.m - m) * c))};
 }
-// Every thread gets the workgroup's; red holds NT / 64 pairs and is free again on return
+// Every thread gets the workgroup's; red holds NT / 64 pairs and is free again on return.  The
+// waves' results are joined by the lanes of each wave (read by every thread for itself, sixteen
+// of them would take the registers of a vector each).
 template <int NT>
 __device__ __forceinline__ Soft block_soft(Soft a, float c, float2* red) {
     a = wave_soft(a, c);
     if constexpr (NT == kWave) return a;
-    constexpr int W = NT / kWave;
-    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = make_float2(a.m, a.s);
+    const int lane = threadIdx.x % kWave;
+    if (lane == 0) red[threadIdx.x / kWave] = make_float2(a.m, a.s);
     __syncthreads();
-    float m = -FLT_MAX, s = 0.f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) m = fmaxf(m, red[w].x);
-#pragma unroll
-    for (int w = 0; w < W; ++w) s += red[w].y * exp2_((red[w].x - m) * c);
+    const float2 r = lane < NT / kWave ? red[lane] : make_float2(-FLT_MAX, 0.f);
     __syncthreads();
-    return {m, s};
+    return wave_soft({r.x, r.y}, c);
 }
 template <int NT>
 __device__ __forceinline__ float block_sum(float x, float* red) {
     x = wave_sum_fast(x);
     if constexpr (NT == kWave) return x;
-    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = x;
+    const int lane = threadIdx.x % kWave;
+    if (lane == 0) red[threadIdx.x / kWave] = x;
     __syncthreads();
-    float s = 0.f;
-#pragma unroll
-    for (int w = 0; w < NT / kWave; ++w) s += red[w];
+    const float r = lane < NT / kWave ? red[lane] : 0.f;
     __syncthreads();
-    return s;
+    return wave_sum_fast(r);
 }
 template <int NT>
 __device__ __forceinline__ float block_max(float x, float* red) {
     x = wave_max_fast(x);
     if constexpr (NT == kWave) return x;
-    if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = x;
+    const int lane = threadIdx.x % kWave;
+    if (lane == 0) red[threadIdx.x / kWave] = x;
     __syncthreads();
-    float m = red[0];
-#pragma unroll
-    for (int w = 1; w < NT / kWave; ++w) m = fmaxf(m, red[w]);
+    const float r = lane < NT / kWave ? red[lane] : -INFINITY;
     __syncthreads();
-    return m;
+    return wave_max_fast(r);
 }
 
 // The same for whole chunks of a row, at one fma, one exponential and one sum a logit: the
@@ -214,6 +221,7 @@ struct ChunkSoft {
     float m, r, s;
     __device__ __forceinline__ void init(float c) { m = -kFar, r = m * c, s = 0.f; }
     __device__ __forceinline__ void raise(float most, float c) {
+#pragma clang fp contract(off)
         if (most > m) {
             const float r2 = most * c;
             s *= exp2_(r - r2);
@@ -223,6 +231,7 @@ struct ChunkSoft {
     }
     template <int W>
     __device__ __forceinline__ void push(const float (&v)[W], float c) {
+#pragma clang fp contract(off)
         float t[W];
 #pragma unroll
         for (int k = 0; k < W; ++k) t[k] = exp2_(fmaf(v[k], c, -r));
@@ -233,6 +242,7 @@ struct ChunkSoft {
         s += t[0];
     }
     __device__ __forceinline__ Soft value(float c) const {
+#pragma clang fp contract(off)
         // 2^(v c - r) = 2^((v - m) c) 2^(m c - r)
         return {s > 0.f ? m : -FLT_MAX, s * exp2_(-fmaf(m, c, -r))};
     }

@@ -12,6 +12,10 @@
 // gradients are  scale * exp(s_v / T - low)  outside the slots, low the log-sum-exp of what was
 // walked over, so one walk over the row gives its sums and a second one writes the gradient,
 // after which the K slots' values are written over it.
+//
+// One workgroup takes a row (k_distill).  For the gradient it reads it again backwards: what was
+// read last is still in the L2, the rest in the memory-side cache.  Where the rows are few each is
+// divided among workgroups, with a launch for the sums (k_distill_sums) and one for what follows.
 #include <hip/hip_runtime.h>
 
 #include "token.h"
@@ -20,8 +24,11 @@ namespace tsc {
 namespace {
 
 constexpr float kMinRest = 9.5367431640625e-7f;   // 2^-20
+constexpr int kPartThreads = 256;
+constexpr int kWantParts = 1024;   // workgroups that fill the chip
+constexpr int kMinPart = 4096;     // tokens of a part
 
-// Slots of a row, held by the workgroup's first kMaxTop threads (a thread has kMaxTop / NT)
+// Slots of a row: a thread has kMaxTop / NT of them, or the first kMaxTop threads one each
 struct Slot {
     int at;    // token, -1: empty
     float t;   // teacher's logit, -inf: empty
@@ -33,144 +40,379 @@ __device__ __forceinline__ float top_value(const void* p, int dtype, int64_t i) 
                                   : to_f(((const F16*)p)[i]);
 }
 
-template <class T, int NT, bool kRest, bool kGrad>
-__global__ __launch_bounds__(NT) void k_distill(DistillArgs a) {
-    extern __shared__ uint32_t marks[];   // kRest: a bit for every token
-    __shared__ float2 red2[16];
-    __shared__ float red[16];
-    constexpr int W = kVec<T>, kSlots = kMaxTop > NT ? kMaxTop / NT : 1;
-    const int tid = threadIdx.x, V = (int)a.V;
-    const float c = a.scale.c, inv_t = a.scale.inv_t;
-    for (int64_t row = blockIdx.x; row < a.B * a.N; row += gridDim.x) {
-        const int64_t b = row / a.N, n = row % a.N;
-        T* grad = (T*)a.grad + row * V;
-        if (n >= clamp_rows(a.lengths, b, a.N)) {
-            if (a.loss && tid == 0) a.loss[row] = 0.f;
-            if constexpr (kGrad)
-                for (int v = tid; v < V; v += NT) grad[v] = from_f<T>(0.f);
-            continue;
-        }
-        const T* x = row_of<T>(a.logits, b, n);
-        // a teacher's row without a finite logit says nothing: its slots are empty
-        const float tl = a.top_lse ? a.top_lse[row] : 0.f;
-        Slot slot[kSlots];
-        float tm = -FLT_MAX;
+// What a row's loss and gradient are made of, the same in every thread
+struct Row {
+    float loss;
+    float low, gain;   // outside the slots: gain * 2^((s_v - low) c)
+    float high, part;  // at slot k: w * (2^((s_k - high) c) * part - p_k)
+    float w;
+};
+
+template <int NT>
+constexpr int kSlots = kMaxTop > NT ? kMaxTop / NT : 1;
+
+template <class T, int NT>
+struct Slots {
+    Slot slot[kSlots<NT>];
+    float xs[kSlots<NT>], p[kSlots<NT>];
+
+    __device__ __forceinline__ void load(const DistillArgs& a, uint32_t row, const T* x, float tl) {
 #pragma unroll
-        for (int q = 0; q < kSlots; ++q) {
-            const int k = q * NT + tid;
+        for (int q = 0; q < kSlots<NT>; ++q) {
+            const int k = q * NT + (int)threadIdx.x;
             slot[q] = {-1, -INFINITY};
+            xs[q] = -INFINITY;
+            // a teacher's row without a finite logit says nothing: its slots are empty
             if (k < a.K && tl != -INFINITY) {
-                const int at = a.top_indices[row * a.K + k];
-                if (at >= 0 && at < V)
-                    slot[q] = {at, top_value(a.top_values, a.top_dtype, row * a.K + k)};
+                const int64_t i = (int64_t)row * a.K + k;
+                const int at = a.top_indices[i];
+                if (at >= 0 && at < (int)a.V) {
+                    slot[q] = {at, top_value(a.top_values, a.top_dtype, i)};
+                    xs[q] = to_f(x[at]);
+                }
             }
-            tm = fmaxf(tm, slot[q].t);
         }
-        if constexpr (kRest) {
-            for (int w = tid; w < (V + 31) / 32; w += NT) marks[w] = 0;
-            __syncthreads();
+    }
+    // Marks the slots of tokens [lo, hi) in bits; every thread calls it, and may read them after
+    __device__ __forceinline__ void mark(uint32_t* bits, int lo, int hi) {
+        for (int w = threadIdx.x; w < (hi - lo + 31) / 32; w += NT) bits[w] = 0;
+        __syncthreads();
 #pragma unroll
-            for (int q = 0; q < kSlots; ++q)
-                if (slot[q].at >= 0) atomicOr(&marks[slot[q].at >> 5], 1u << (slot[q].at & 31));
-            __syncthreads();
+        for (int q = 0; q < kSlots<NT>; ++q) {
+            const int at = slot[q].at - lo;
+            if (at >= 0 && at < hi - lo) atomicOr(&bits[at >> 5], 1u << (at & 31));
         }
-        Soft soft = soft_empty();
-        walk_row<T, NT, 4>(x, 0, V, tid, [&](const float (&v)[W], int at, int) {
-            if constexpr (kRest) {
-                const uint32_t bits = marks[at >> 5] >> (at & 31);   // at is a multiple of W
-                float u[W];
-#pragma unroll
-                for (int k = 0; k < W; ++k) u[k] = bits >> k & 1 ? -INFINITY : v[k];
-                soft_push(soft, u, c);
-            } else {
-                soft_push(soft, v, c);
-            }
-        });
-        soft = block_soft<NT>(soft, c, red2);
-        // the slots: teacher's p, student's numerators at the common maximum
-        float xs[kSlots], p[kSlots];
-        Soft own = soft_empty();
-#pragma unroll
-        for (int q = 0; q < kSlots; ++q) {
-            xs[q] = slot[q].at >= 0 ? to_f(x[slot[q].at]) : -INFINITY;
-            own.m = fmaxf(own.m, xs[q]);
-        }
+        __syncthreads();
+    }
+    // soft: of the tokens walked over (all, or with a rest those outside the slots)
+    template <bool kRest>
+    __device__ Row finish(const DistillArgs& a, uint32_t row, Soft soft, float tl, float2* red) {
+#pragma clang fp contract(off)   // the loss is the same with the gradient and without, to the bit
+        const float c = a.scale.c, inv_t = a.scale.inv_t;
+        float* redf = (float*)red;
         Soft all = soft;
         if constexpr (kRest) {
+            Soft own = soft_empty();
 #pragma unroll
-            for (int q = 0; q < kSlots; ++q) own.s += exp2_((xs[q] - own.m) * c);
-            all = soft_merge(soft, block_soft<NT>(own, c, red2), c);
+            for (int q = 0; q < kSlots<NT>; ++q) own.m = fmaxf(own.m, xs[q]);
+#pragma unroll
+            for (int q = 0; q < kSlots<NT>; ++q) own.s += exp2_((xs[q] - own.m) * c);
+            all = soft_merge(soft, block_soft<NT>(own, c, red), c);
         }
-        float norm;
-        if (a.top_lse) {
+        float norm = 1.f;
+        if (kRest) {
 #pragma unroll
-            for (int q = 0; q < kSlots; ++q)
+            for (int q = 0; q < kSlots<NT>; ++q)
                 p[q] = slot[q].at >= 0 ? exp_(slot[q].t * inv_t - tl) : 0.f;
-            norm = 1.f;
         } else {
-            tm = block_max<NT>(tm, red);
-            float s = 0.f;
+            float tm = -FLT_MAX, s = 0.f;
 #pragma unroll
-            for (int q = 0; q < kSlots; ++q) s += p[q] = exp2_((slot[q].t - tm) * c);
-            s = block_sum<NT>(s, red);
+            for (int q = 0; q < kSlots<NT>; ++q) tm = fmaxf(tm, slot[q].t);
+            tm = block_max<NT>(tm, redf);
+#pragma unroll
+            for (int q = 0; q < kSlots<NT>; ++q) s += p[q] = exp2_((slot[q].t - tm) * c);
+            s = block_sum<NT>(s, redf);
             norm = s > 0.f ? 1.f / s : 0.f;
         }
         float mass = 0.f, kl = 0.f;
         const float ls = all.s > 0.f ? logf(all.s) : 0.f;
 #pragma unroll
-        for (int q = 0; q < kSlots; ++q) {
+        for (int q = 0; q < kSlots<NT>; ++q) {
             p[q] *= norm;
             if (p[q] > 0.f) {
                 mass += p[q];
                 kl += p[q] * (logf(p[q]) - ((xs[q] - all.m) * inv_t - ls));
             }
         }
-        mass = block_sum<NT>(mass, red);
-        kl = block_sum<NT>(kl, red);
-        float keep = mass > 0.f ? 1.f : 0.f;   // outside the slots: keep * exp(s_v / T - low)
+        mass = block_sum<NT>(mass, redf);
+        kl = block_sum<NT>(kl, redf);
+        float keep = mass > 0.f ? 1.f : 0.f;
         if constexpr (kRest) {
             float rest = 1.f - mass;
             if (!(rest > kMinRest)) rest = 0.f;
-            const float low = soft.s > 0.f ? (soft.m - all.m) * inv_t + logf(soft.s) - ls : -INFINITY;
+            const float low =
+                soft.s > 0.f ? (soft.m - all.m) * inv_t + logf(soft.s) - ls : -INFINITY;
             if (rest > 0.f) kl += rest * (logf(rest) - low);
             keep = exp_(low) - rest;
         }
-        if (a.loss && tid == 0) a.loss[row] = kl;
-        if constexpr (kGrad) {
-            const float w = (a.weights ? a.weights[row] : 1.f) * inv_t;
-            const float g = soft.s > 0.f ? w * keep / soft.s : 0.f;
-            const float m = soft.m;
-            walk_row<T, NT, 4>(x, 0, V, tid, [&](const float (&v)[W], int at, int num) {
-                float y[W];
+        Row r;
+        r.loss = kl;
+        r.w = all.s > 0.f ? (a.weights ? a.weights[row] : 1.f) * inv_t : 0.f;
+        r.low = soft.m;
+        r.gain = soft.s > 0.f ? r.w * keep / soft.s : 0.f;
+        r.high = all.m;
+        r.part = all.s > 0.f && (kRest || keep > 0.f) ? 1.f / all.s : 0.f;
+        return r;
+    }
+    // The gradient at the slots of tokens [lo, hi); the walk's values there are written before
+    __device__ __forceinline__ void write(const Row& r, float c, T* grad, int lo, int hi) {
+        __syncthreads();
 #pragma unroll
-                for (int k = 0; k < W; ++k) y[k] = g * exp2_((v[k] - m) * c);
-                if (num == W)
-                    *(Raw<T>*)(grad + at) = pack<T>(y);
-                else
-                    grad[at] = from_f<T>(y[0]);
-            });
-            __syncthreads();   // the slots' values come after the walk's
+        for (int q = 0; q < kSlots<NT>; ++q)
+            if (slot[q].at >= lo && slot[q].at < hi)
+                grad[slot[q].at] = from_f<T>(r.w * (exp2_((xs[q] - r.high) * c) * r.part - p[q]));
+    }
+};
+
+// A vector's logits, -inf at the slots
+template <class T, bool kRest>
+__device__ __forceinline__ void unslotted(const Raw<T>& r, const uint32_t* bits, int at,
+                                          float (&v)[kVec<T>]) {
+    unpack<T>(r, v);
+    if constexpr (kRest) {
+        const uint32_t m = bits[at >> 5] >> (at & 31) & ((1u << kVec<T>) - 1);
+        if (m)
 #pragma unroll
-            for (int q = 0; q < kSlots; ++q)
-                if (slot[q].at >= 0) {
-                    const float qk =
-                        all.s > 0.f ? exp2_((xs[q] - all.m) * c) / all.s * (kRest || keep > 0.f) : 0.f;
-                    grad[slot[q].at] = from_f<T>(w * (qk - (all.s > 0.f ? p[q] : 0.f)));
-                }
+            for (int k = 0; k < kVec<T>; ++k) v[k] = m >> k & 1 ? -INFINITY : v[k];
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void store_grad(T* grad, const Raw<T>& r, const Row& row, float c) {
+    float v[kVec<T>];
+    unpack<T>(r, v);
+#pragma unroll
+    for (int k = 0; k < kVec<T>; ++k) v[k] = row.gain * exp2_((v[k] - row.low) * c);
+    store_raw<T>(grad, pack<T>(v));
+}
+
+template <class T, int NT>
+__device__ __forceinline__ void write_zeros(T* grad, int lo, int hi) {
+    const int nv = (hi - lo) / kVec<T>;
+    for (int i = threadIdx.x; i < nv; i += NT) store_raw<T>(grad + lo + (size_t)i * kVec<T>, Raw<T>{});
+    const int e = lo + nv * kVec<T> + (int)threadIdx.x;
+    if (e < hi) grad[e] = from_f<T>(0.f);
+}
+
+// Maximum and sum of tokens [lo, hi) outside the slots, the slow way that any logits allow
+template <class T, int NT, bool kRest>
+__device__ Soft sums_again(const T* x, const uint32_t* bits, int lo, int hi, float c, float2* red) {
+    constexpr int W = kVec<T>;
+    Soft s = soft_empty();
+    walk_row<T, NT, 1>(x, lo, hi, threadIdx.x, [&](float (&v)[W], int at, int) {
+        if constexpr (kRest) {
+#pragma unroll
+            for (int k = 0; k < W; ++k) {
+                const int e = min(at + k, hi - 1) - lo;
+                v[k] = bits[e >> 5] >> (e & 31) & 1 ? -INFINITY : v[k];
+            }
         }
-        __syncthreads();   // marks are free for the next row
+        soft_push(s, v, c);
+    });
+    return block_soft<NT>(s, c, red);
+}
+
+template <class T, int NT, bool kRest, bool kGrad>
+__global__ __launch_bounds__(NT) void k_distill(DistillArgs a) {
+    extern __shared__ uint32_t bits[];   // kRest: a bit for every token
+    __shared__ float2 red[8];
+    constexpr int W = kVec<T>, kU = kGrad ? 2 : 4;   // vectors asked for at once
+    const int tid = threadIdx.x, V = (int)a.V, nv = V / W;
+    const float c = a.scale.c;
+    const uint32_t rows = (uint32_t)(a.B * a.N), N = (uint32_t)a.N;
+    for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const uint32_t b = row / N, n = row % N;
+        T* grad = (T*)a.grad + (size_t)row * V;
+        if (n >= clamp_rows(a.lengths, b, N)) {
+            if (a.loss && tid == 0) a.loss[row] = 0.f;
+            if constexpr (kGrad) write_zeros<T, NT>(grad, 0, V);
+            continue;
+        }
+        const T* x = row_of<T>(a.logits, b, n);
+        // (a vector's place as a 32-bit offset from the row's: one register and not two)
+        auto from = [&](int i) { return (const T*)((const char*)x + (uint32_t)i * 16u); };
+        auto to = [&](int i) { return (T*)((char*)grad + (uint32_t)i * 16u); };
+        const float tl = kRest ? a.top_lse[row] : 0.f;
+        Slots<T, NT> slots;
+        slots.load(a, row, x, tl);
+        if constexpr (kRest) slots.mark(bits, 0, V);
+        ChunkSoft soft;
+        soft.init(c);
+        float most = -INFINITY;
+        auto push = [&](const Raw<T>& r, int i) {
+            float v[W];
+            unslotted<T, kRest>(r, bits, i * W, v);
+            const float t = max_of(v);
+            most = fmaxf(most, t);
+            soft.raise(t, c);
+            soft.push(v, c);
+        };
+        int i = tid;
+        for (; i + (kU - 1) * NT < nv; i += kU * NT) {
+            Raw<T> r[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u) r[u] = load_raw<T, !kGrad>(from(i + u * NT));
+#pragma unroll
+            for (int u = 0; u < kU; ++u) push(r[u], i + u * NT);
+        }
+        for (; i < nv; i += NT) push(load_raw<T, !kGrad>(from(i)), i);
+        const int e = nv * W + tid;   // the row's last few tokens
+        if (e < V) {
+            float one[1] = {kRest && bits[e >> 5] >> (e & 31) & 1 ? -INFINITY : to_f(x[e])};
+            most = fmaxf(most, one[0]);
+            soft.raise(one[0], c);
+            soft.push(one, c);
+        }
+        Soft all = block_soft<NT>(soft.value(c), c, red);
+        if (far(block_max<NT>(most, (float*)red)))
+            all = sums_again<T, NT, kRest>(x, bits, 0, V, c, red);
+        const Row r = slots.template finish<kRest>(a, row, all, tl, red);
+        if (a.loss && tid == 0) a.loss[row] = r.loss;
+        if constexpr (kGrad) {
+            if (e < V) grad[e] = from_f<T>(r.gain * exp2_((to_f(x[e]) - r.low) * c));
+            // backwards: what was read last is nearest
+            i = tid + (nv > tid ? (nv - 1 - tid) / NT * NT : -NT);
+            for (; i - (kU - 1) * NT >= 0; i -= kU * NT) {
+                Raw<T> q[kU];
+#pragma unroll
+                for (int u = 0; u < kU; ++u) q[u] = load_raw<T, true>(from(i - u * NT));
+#pragma unroll
+                for (int u = 0; u < kU; ++u) store_grad<T>(to(i - u * NT), q[u], r, c);
+            }
+            for (; i >= 0; i -= NT)
+                store_grad<T>(to(i), load_raw<T, true>(from(i)), r, c);
+            slots.write(r, c, grad, 0, V);
+        }
+        __syncthreads();   // bits are free for the next row
+    }
+}
+
+// ---- few rows ----
+
+struct DistillPlan {
+    int parts;
+    float4* sums;   // [rows][parts]: maximum and sum, largest logit
+    size_t bytes;
+};
+DistillPlan distill_plan(int64_t rows, int64_t V, void* ws) {
+    DistillPlan p;
+    int64_t parts = (kWantParts + rows - 1) / rows;
+    const int64_t most = (V + kMinPart - 1) / kMinPart;
+    if (parts > most) parts = most;
+    if (parts > kWave) parts = kWave;
+    p.parts = (int)parts;
+    p.sums = (float4*)ws;
+    p.bytes = parts > 1 ? ((size_t)rows * parts * sizeof(float4) + 255) / 256 * 256 : 0;
+    return p;
+}
+// Tokens [lo, hi) of a part: a multiple of 64, so that parts of an aligned row are aligned
+__device__ __forceinline__ void part_range(int V, int parts, int part, int* lo, int* hi) {
+    const int per = ((V + parts - 1) / parts + 63) / 64 * 64;
+    *lo = min(part * per, V);
+    *hi = min(*lo + per, V);
+}
+
+template <class T, bool kRest>
+__global__ __launch_bounds__(kPartThreads) void k_distill_sums(DistillArgs a, DistillPlan p) {
+    extern __shared__ uint32_t bits[];
+    __shared__ float2 red[kPartThreads / kWave];
+    constexpr int NT = kPartThreads, W = kVec<T>;
+    const uint32_t row = blockIdx.x / (uint32_t)p.parts, part = blockIdx.x % (uint32_t)p.parts;
+    const uint32_t b = row / (uint32_t)a.N, n = row % (uint32_t)a.N;
+    if (n >= clamp_rows(a.lengths, b, a.N)) return;
+    const T* x = row_of<T>(a.logits, b, n);
+    const float c = a.scale.c;
+    int lo, hi;
+    part_range((int)a.V, p.parts, part, &lo, &hi);
+    if constexpr (kRest) {
+        Slots<T, NT> slots;
+        slots.load(a, row, x, a.top_lse[row]);
+        slots.mark(bits, lo, hi);
+    }
+    ChunkSoft soft;
+    soft.init(c);
+    float most = -INFINITY;
+    walk_row<T, NT, 4>(x, lo, hi, threadIdx.x, [&](float (&v)[W], int at, int num) {
+        if constexpr (kRest) {
+            const uint32_t m = bits[(at - lo) >> 5] >> ((at - lo) & 31) & ((1u << W) - 1);
+            if (m)
+#pragma unroll
+                for (int k = 0; k < W; ++k) v[k] = m >> k & 1 ? -INFINITY : v[k];
+        }
+        const float t = max_of(v);
+        most = fmaxf(most, t);
+        soft.raise(t, c);
+        soft.push(v, c);
+    });
+    Soft s = block_soft<NT>(soft.value(c), c, red);
+    most = block_max<NT>(most, (float*)red);
+    if (most != -INFINITY && far(most)) s = sums_again<T, NT, kRest>(x, bits, lo, hi, c, red);
+    if (threadIdx.x == 0) p.sums[blockIdx.x] = make_float4(s.m, s.s, most, 0.f);
+}
+
+template <class T, bool kRest, bool kGrad>
+__global__ __launch_bounds__(kPartThreads) void k_distill_parts(DistillArgs a, DistillPlan p) {
+    __shared__ float2 red[kPartThreads / kWave];
+    constexpr int NT = kPartThreads, W = kVec<T>;
+    const uint32_t parts = kGrad ? (uint32_t)p.parts : 1;
+    const uint32_t row = blockIdx.x / parts, part = blockIdx.x % parts;
+    const uint32_t b = row / (uint32_t)a.N, n = row % (uint32_t)a.N;
+    T* grad = (T*)a.grad + (size_t)row * a.V;
+    int lo, hi;
+    part_range((int)a.V, p.parts, part, &lo, &hi);
+    if (n >= clamp_rows(a.lengths, b, a.N)) {
+        if (a.loss && part == 0 && threadIdx.x == 0) a.loss[row] = 0.f;
+        if constexpr (kGrad) write_zeros<T, NT>(grad, lo, hi);
+        return;
+    }
+    const T* x = row_of<T>(a.logits, b, n);
+    const float c = a.scale.c, tl = kRest ? a.top_lse[row] : 0.f;
+    Slots<T, NT> slots;
+    slots.load(a, row, x, tl);
+    const int lane = threadIdx.x % kWave;
+    const float4 s = lane < p.parts ? p.sums[(size_t)row * p.parts + lane]
+                                    : make_float4(-FLT_MAX, 0.f, 0.f, 0.f);
+    const Row r = slots.template finish<kRest>(a, row, wave_soft({s.x, s.y}, c), tl, red);
+    if (a.loss && part == 0 && threadIdx.x == 0) a.loss[row] = r.loss;
+    if constexpr (kGrad) {
+        walk_row<T, NT, 4, true>(x, lo, hi, threadIdx.x, [&](const float (&v)[W], int at, int num) {
+            float y[W];
+#pragma unroll
+            for (int k = 0; k < W; ++k) y[k] = r.gain * exp2_((v[k] - r.low) * c);
+            if (num == W)
+                store_raw<T>(grad + at, pack<T>(y));
+            else
+                grad[at] = from_f<T>(y[0]);
+        });
+        slots.write(r, c, grad, lo, hi);
     }
 }
 
 }  // namespace
 
-size_t distill_workspace(int, int64_t, int64_t, int64_t, int64_t) { return 0; }
+size_t distill_workspace(int, int64_t B, int64_t N, int64_t V, int64_t) {
+    return distill_plan(B * N, V, nullptr).bytes;
+}
 
 hipError_t launch_distill(const DistillArgs& a, hipStream_t s) {
+    hipError_t e = hipSuccess;
     with_type(a.dtype, [&](auto t) {
         using T = decltype(t);
         const int64_t rows = a.B * a.N;
-        const size_t lds = a.top_lse ? (size_t)(a.V + 31) / 32 * 4 : 0;
+        const int V = (int)a.V;
+        const DistillPlan p = distill_plan(rows, V, a.ws);
+        if (p.parts > 1) {
+            const unsigned grid = (unsigned)(rows * p.parts), one = (unsigned)rows;
+            // bits of a part's tokens
+            const size_t lds = ((size_t)(V + p.parts - 1) / p.parts + 63) / 64 * 64 / 8;
+            if (a.top_lse) {
+                k_distill_sums<T, true><<<grid, kPartThreads, lds, s>>>(a, p);
+                if ((e = hipGetLastError()) != hipSuccess) return;
+                if (a.grad)
+                    k_distill_parts<T, true, true><<<grid, kPartThreads, 0, s>>>(a, p);
+                else
+                    k_distill_parts<T, true, false><<<one, kPartThreads, 0, s>>>(a, p);
+            } else {
+                k_distill_sums<T, false><<<grid, kPartThreads, 0, s>>>(a, p);
+                if ((e = hipGetLastError()) != hipSuccess) return;
+                if (a.grad)
+                    k_distill_parts<T, false, true><<<grid, kPartThreads, 0, s>>>(a, p);
+                else
+                    k_distill_parts<T, false, false><<<one, kPartThreads, 0, s>>>(a, p);
+            }
+            return;
+        }
+        const size_t lds = a.top_lse ? (size_t)(V + 31) / 32 * 4 : 0;
         auto go = [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
             const unsigned g = row_grid(rows, NT);
@@ -183,14 +425,14 @@ hipError_t launch_distill(const DistillArgs& a, hipStream_t s) {
             else
                 k_distill<T, NT, false, false><<<g, NT, 0, s>>>(a);
         };
-        if (a.V <= 1024)
+        if (V <= 1024)
             go(std::integral_constant<int, 64>{});
-        else if (a.V <= 8192)
+        else if (V <= 8192)
             go(std::integral_constant<int, 256>{});
         else
-            go(std::integral_constant<int, 1024>{});
+            go(std::integral_constant<int, 512>{});
     });
-    return hipGetLastError();
+    return e == hipSuccess ? hipGetLastError() : e;
 }
 
 }  // namespace tsc
