@@ -425,9 +425,12 @@ hipError_t launch_distill(const DistillArgs& a, hipStream_t s) {
             else
                 k_distill<T, NT, false, false><<<g, NT, 0, s>>>(a);
         };
-        if (V <= 1024)
+        // A wave a row while the rows fill the chip so: its sums need no barrier.  Gradients of 64
+        // slots, us a call by 64 / 256 / 512 threads: 16384 rows of 1100 33 / 75 / 136, 8192 of 8000
+        // 77 / 80 / 96, 4096 of 16000 71 / 66 / 72, 2048 of 32000 75 / 66 / 63.
+        if (V <= 1024 || (V <= 8192 && rows >= 2048))
             go(std::integral_constant<int, 64>{});
-        else if (V <= 8192)
+        else if (V <= 24576)
             go(std::integral_constant<int, 256>{});
         else
             go(std::integral_constant<int, 512>{});

@@ -445,26 +445,26 @@ __global__ __launch_bounds__(kScanThreads, 8) void k_top_scan(TopArgs a, TopPlan
     };
     const char* base = (const char*)x;
     auto load = [&](int v) { return load_raw<T, true>((const T*)(base + (uint32_t)v * 16u)); };
-    int v = lo + tid;
-    for (; v + 3 * NT < hi; v += 4 * NT) {
+    // the loops go by the wave's first lane, so that all its lanes count the same vectors
+    int v = __builtin_amdgcn_readfirstlane(lo + wave * kWave);
+    for (; v + 3 * NT + kWave <= hi; v += 4 * NT) {
+        const int i = v + lane;
         Raw<T> r[2], s[2];
-        r[0] = load(v), r[1] = load(v + NT), s[0] = load(v + 2 * NT), s[1] = load(v + 3 * NT);
-        work(r, v, v + NT);
-        work(s, v + 2 * NT, v + 3 * NT);
+        r[0] = load(i), r[1] = load(i + NT), s[0] = load(i + 2 * NT), s[1] = load(i + 3 * NT);
+        work(r, i, i + NT);
+        work(s, i + 2 * NT, i + 3 * NT);
     }
-    // a wave's first lane is in every turn that any of its lanes is in, and has counted them all
-    found = __builtin_amdgcn_readfirstlane(found);
     for (; v < hi; v += NT) {
-        Raw<T> r[2] = {load(v), {}};
+        const int i = v + lane;
+        const Raw<T> r = load(min(i, hi - 1));
         float one[W];
-        unpack<T>(r[0], one);
-        const float t = max_of(one);
+        unpack<T>(r, one);
+        const float t = i < hi ? max_of(one) : -INFINITY;
         most = fmaxf(most, t);
         soft.raise(t, c);
-        soft.push(one, c);
-        keep(t >= least, r[0], v);
+        if (i < hi) soft.push(one, c);
+        keep(t >= least, r, i);
     }
-    found = __builtin_amdgcn_readfirstlane(found);
     const int e = nv * W + tid;   // the row's last few logits; k_top_pick looks at all of them
     if (part == 0 && e < a.V) {
         float one[1] = {to_f(x[e])};

@@ -95,6 +95,19 @@ def test_large_logits_together(V, K):
     _check(x, K, tag="together")
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("V", [1025, 1500, 2047, 3001, 6151, 8200, 9000, 12345, 20008, 32000, 36860])
+def test_rows_that_end_within_a_wave(V, dtype):
+    # the K largest spread over the row's last few thousand logits, in rows whose last vectors are
+    # those of a part of a wave, and enough rows that none is divided
+    x = _normal((1, 2100, V), dtype, V)
+    x[0, :, max(0, V - 3000):] += 6
+    few = x[:, ::300].contiguous()
+    _check(few, 40, tag="ends")
+    for a, b in zip(_run(x, 40)[:2], _run(few, 40)[:2]):
+        assert bool((a[:, ::300] == b).all())
+
+
 @pytest.mark.parametrize("T", [0.1, 0.7, 3.0])
 def test_temperature(T):
     _check(_normal((1, 3, 9001), "float16", 5), 20, T=T, tag="temperature")
