@@ -24,7 +24,7 @@ constexpr int kMaxParts = kWave;   // parts of a row: one a lane when they are j
 constexpr int kMinPart = 2048;     // elements of a part: 8 a thread
 constexpr int kMaxGroups = 8;      // launches that the positions are divided among
 constexpr int kAlive = 0x7fffffff;
-constexpr double kApartElems = 8e6;   // elements of a position's rows from which it has a launch
+constexpr double kApartElems = 16e6;   // elements of a position's rows from which it has a launch
 constexpr int kStatParts = 2048, kDrawParts = 1024;   // workgroups that fill the chip
 
 // Parts of a row: enough workgroups to fill the chip where the rows are few
@@ -459,11 +459,12 @@ hipError_t launch_verify(const VerifyArgs& a, hipStream_t s) {
                 return;
             }
             const Plan p = plan_of(a.B, a.G, a.V, a.ws);
-            // positions [0, 1), [1, 2), [2, 4), [4, 8) ... where a position is worth a launch
+            // positions [0, 2), [2, 5), [5, 11) ... where they are worth a launch, 64 at most for
+            // the tests of the next
             int64_t before = 0, t0 = 0;
             for (int group = 0; t0 <= a.G; ++group) {
                 int64_t t1 = a.G + 1;
-                if (p.apart && group < kMaxGroups - 1) t1 = min(t1, t0 + (t0 > 1 ? t0 : 1));
+                if (p.apart && group < kMaxGroups - 1) t1 = min(t1, t0 + (t0 < 1 ? 2 : t0 < 63 ? t0 + 1 : 64));
                 k_verify_stats<TT, TD>
                     <<<row_grid(a.B * 2 * (t1 - t0) * p.parts, kStatThreads), kStatThreads, 0, s>>>(
                         a, p, before, t0, t1, group);
