@@ -28,6 +28,7 @@ constexpr int kSmallThreads = 1024;
 constexpr int kSmallElems = 4096;
 constexpr int kMaxParts = kWave;   // parts of a row: one a lane when they are joined
 constexpr int kMinPart = 2048;     // elements of a part: 8 a thread
+constexpr int kMaxPart = 32768;
 constexpr int kMaxGroups = 8;      // launches that the positions are divided among
 constexpr int kAlive = 0x7fffffff;
 // Elements of a position's rows from which the positions are divided among launches (us undivided /
@@ -36,9 +37,12 @@ constexpr int kAlive = 0x7fffffff;
 constexpr double kApartElems = 16e6;
 constexpr int kStatParts = 2048, kDrawParts = 1024;   // workgroups that fill the chip
 
-// Parts of a row: enough workgroups to fill the chip where the rows are few
+// Parts of a row: enough workgroups to fill the chip where the rows are few, and none so long that
+// the chip waits for the last of them where sequences have unequal numbers of drafts (128
+// sequences of up to 8 over 100003 tokens: 97 us in whole rows, 88 in quarters)
 inline int parts_of(int64_t rows, int64_t V, int64_t want) {
     int64_t p = (want + rows - 1) / rows;
+    if (p < (V + kMaxPart - 1) / kMaxPart) p = (V + kMaxPart - 1) / kMaxPart;
     const int64_t most = (V + kMinPart - 1) / kMinPart;
     if (p > most) p = most;
     if (p > kMaxParts) p = kMaxParts;
@@ -158,10 +162,12 @@ __global__ __launch_bounds__(kStatThreads) void k_verify_stats(VerifyArgs a, Pla
                                                                int64_t t0, int64_t t1, int group) {
     __shared__ float2 red[kStatThreads / kWave];
     __shared__ Tests sh;
-    // 32-bit divisions: parts * rows stay below 2^32 (a row has parts only where rows are few)
-    const uint32_t width = 2 * (uint32_t)(t1 - t0), items = (uint32_t)(p.parts * a.B * width);
-    for (uint32_t i = blockIdx.x; i < items; i += gridDim.x) {
-        const uint32_t row_at = i / (uint32_t)p.parts, part = i % (uint32_t)p.parts;
+    const uint32_t width = 2 * (uint32_t)(t1 - t0);
+    const uint64_t items = (uint64_t)p.parts * a.B * width;
+    for (uint64_t i = blockIdx.x; i < items; i += gridDim.x) {
+        // (64-bit divisions take as long as a small part)
+        const uint32_t row_at = items >> 32 ? (uint32_t)(i / p.parts) : (uint32_t)i / (uint32_t)p.parts;
+        const uint32_t part = (uint32_t)(i - (uint64_t)row_at * p.parts);
         const int64_t b = row_at / width;
         const uint32_t r = row_at % width;
         const int64_t t = t0 + r / 2;
@@ -268,10 +274,11 @@ __global__ __launch_bounds__(kDrawThreads) void k_verify_draw(VerifyArgs a, Plan
     __shared__ Tests sh;
     __shared__ uint64_t words[kDrawThreads / kWave];
     const int tid = threadIdx.x;
-    const uint32_t items = (uint32_t)(p.draw_parts * a.B);
-    for (uint32_t i = blockIdx.x; i < items; i += gridDim.x) {
-        const int64_t b = i / (uint32_t)p.draw_parts;
-        const int part = (int)(i % (uint32_t)p.draw_parts);
+    const uint64_t items = (uint64_t)p.draw_parts * a.B;
+    for (uint64_t i = blockIdx.x; i < items; i += gridDim.x) {
+        const int64_t b = items >> 32 ? (int64_t)(i / p.draw_parts)
+                                      : (int64_t)((uint32_t)i / (uint32_t)p.draw_parts);
+        const int part = (int)(i - (uint64_t)b * p.draw_parts);
         const int64_t n = clamp_rows(a.lengths, b, a.G);
         int32_t* out = a.out + b * (a.G + 1);
         float* logp = a.logp ? a.logp + b * (a.G + 1) : nullptr;
