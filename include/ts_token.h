@@ -99,7 +99,8 @@ ts_status ts_token_distill(const void* logits, int dtype, int64_t stride_b, int6
  *   weights  float32 [B, N] or NULL (all 1): the derivative of what is minimised by each row's
  *            loss (1 / rows for a mean; T^2 / rows to keep the scale of T = 1).
  *   loss     float32 [B, N] or NULL: as above, not weighted.
- *   grad     [B, N, V], contiguous, of the logits' type: weights * d loss / d logits,
+ *   grad     [B, N, V], contiguous, of the logits' type, not overlapping them:
+ *            weights * d loss / d logits,
  *              weights / T * (q_v sum_k p_k - p_v)      without top_lse,
  *              weights / T * (q_v - p_v)                with it, at the slots' tokens,
  *              weights / T * q_v (1 - p_r / q_r)        with it, elsewhere,

@@ -276,6 +276,12 @@ __device__ __forceinline__ const T* row_of(const Rows& x, int64_t b, int64_t n) 
     return (const T*)x.p + b * x.sb + n * x.sn;
 }
 
+// i / d of an item i < items: in 32 bits where they do, as 64-bit divisions take as long as a small
+// part of a row
+__device__ __forceinline__ uint32_t item_row(uint64_t i, int d, uint64_t items) {
+    return items >> 32 ? (uint32_t)(i / (uint64_t)d) : (uint32_t)i / (uint32_t)d;
+}
+
 // A launch holds fewer than 2^32 threads: kernels walk the rows with this many workgroups
 inline unsigned row_grid(int64_t rows, int threads) {
     const int64_t most = (int64_t)0xffffffff / threads;

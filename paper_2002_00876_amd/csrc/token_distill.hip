@@ -30,6 +30,7 @@ constexpr float kMinRest = 9.5367431640625e-7f;   // 2^-20
 constexpr int kPartThreads = 256;
 constexpr int kWantParts = 1024;   // workgroups that fill the chip
 constexpr int kMinPart = 4096;     // tokens of a part
+constexpr int kMaxPart = 262144;   // whose marks take half of a workgroup's 64 KiB of LDS
 
 // Slots of a row: a thread has kMaxTop / NT of them, or the first kMaxTop threads one each
 struct Slot {
@@ -293,6 +294,7 @@ DistillPlan distill_plan(int64_t rows, int64_t V, void* ws) {
     const int64_t most = (V + kMinPart - 1) / kMinPart;
     if (parts > most) parts = most;
     if (parts > kWave) parts = kWave;
+    if (parts < (V + kMaxPart - 1) / kMaxPart) parts = (V + kMaxPart - 1) / kMaxPart;
     p.parts = (int)parts;
     p.sums = (float4*)ws;
     p.bytes = parts > 1 ? ((size_t)rows * parts * sizeof(float4) + 255) / 256 * 256 : 0;
@@ -310,74 +312,83 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_sums(DistillArgs a, Di
     extern __shared__ uint32_t bits[];
     __shared__ float2 red[kPartThreads / kWave];
     constexpr int NT = kPartThreads, W = kVec<T>;
-    const uint32_t row = blockIdx.x / (uint32_t)p.parts, part = blockIdx.x % (uint32_t)p.parts;
-    const uint32_t b = row / (uint32_t)a.N, n = row % (uint32_t)a.N;
-    if (n >= clamp_rows(a.lengths, b, a.N)) return;
-    const T* x = row_of<T>(a.logits, b, n);
-    const float c = a.scale.c;
-    int lo, hi;
-    part_range((int)a.V, p.parts, part, &lo, &hi);
-    if constexpr (kRest) {
-        Slots<T, NT> slots;
-        slots.load(a, row, x, a.top_lse[row]);
-        slots.mark(bits, lo, hi);
-    }
-    ChunkSoft soft;
-    soft.init(c);
-    float most = -INFINITY;
-    walk_row<T, NT, 4>(x, lo, hi, threadIdx.x, [&](float (&v)[W], int at, int num) {
+    const uint64_t items = (uint64_t)(a.B * a.N) * p.parts;
+    for (uint64_t i = blockIdx.x; i < items; i += gridDim.x) {
+        const uint32_t row = item_row(i, p.parts, items);
+        const int part = (int)(i - (uint64_t)row * p.parts);
+        const uint32_t b = row / (uint32_t)a.N, n = row % (uint32_t)a.N;
+        if (n >= clamp_rows(a.lengths, b, a.N)) continue;
+        const T* x = row_of<T>(a.logits, b, n);
+        const float c = a.scale.c;
+        int lo, hi;
+        part_range((int)a.V, p.parts, part, &lo, &hi);
         if constexpr (kRest) {
-            const uint32_t m = bits[(at - lo) >> 5] >> ((at - lo) & 31) & ((1u << W) - 1);
-            if (m)
-#pragma unroll
-                for (int k = 0; k < W; ++k) v[k] = m >> k & 1 ? -INFINITY : v[k];
+            Slots<T, NT> slots;
+            slots.load(a, row, x, a.top_lse[row]);
+            slots.mark(bits, lo, hi);
         }
-        const float t = max_of(v);
-        most = fmaxf(most, t);
-        soft.raise(t, c);
-        soft.push(v, c);
-    });
-    Soft s = block_soft<NT>(soft.value(c), c, red);
-    most = block_max<NT>(most, (float*)red);
-    if (most != -INFINITY && far(most)) s = sums_again<T, NT, kRest>(x, bits, lo, hi, c, red);
-    if (threadIdx.x == 0) p.sums[blockIdx.x] = make_float4(s.m, s.s, most, 0.f);
+        ChunkSoft soft;
+        soft.init(c);
+        float most = -INFINITY;
+        walk_row<T, NT, 4>(x, lo, hi, threadIdx.x, [&](float (&v)[W], int at, int num) {
+            if constexpr (kRest) {
+                const uint32_t m = bits[(at - lo) >> 5] >> ((at - lo) & 31) & ((1u << W) - 1);
+                if (m)
+#pragma unroll
+                    for (int k = 0; k < W; ++k) v[k] = m >> k & 1 ? -INFINITY : v[k];
+            }
+            const float t = max_of(v);
+            most = fmaxf(most, t);
+            soft.raise(t, c);
+            soft.push(v, c);
+        });
+        Soft s = block_soft<NT>(soft.value(c), c, red);
+        most = block_max<NT>(most, (float*)red);
+        if (most != -INFINITY && far(most)) s = sums_again<T, NT, kRest>(x, bits, lo, hi, c, red);
+        if (threadIdx.x == 0) p.sums[i] = make_float4(s.m, s.s, most, 0.f);
+        __syncthreads();   // bits are free for the next part
+    }
 }
 
 template <class T, bool kRest, bool kGrad>
 __global__ __launch_bounds__(kPartThreads) void k_distill_parts(DistillArgs a, DistillPlan p) {
     __shared__ float2 red[kPartThreads / kWave];
     constexpr int NT = kPartThreads, W = kVec<T>;
-    const uint32_t parts = kGrad ? (uint32_t)p.parts : 1;
-    const uint32_t row = blockIdx.x / parts, part = blockIdx.x % parts;
-    const uint32_t b = row / (uint32_t)a.N, n = row % (uint32_t)a.N;
-    T* grad = (T*)a.grad + (size_t)row * a.V;
-    int lo, hi;
-    part_range((int)a.V, p.parts, part, &lo, &hi);
-    if (n >= clamp_rows(a.lengths, b, a.N)) {
-        if (a.loss && part == 0 && threadIdx.x == 0) a.loss[row] = 0.f;
-        if constexpr (kGrad) write_zeros<T, NT>(grad, lo, hi);
-        return;
-    }
-    const T* x = row_of<T>(a.logits, b, n);
-    const float c = a.scale.c, tl = kRest ? a.top_lse[row] : 0.f;
-    Slots<T, NT> slots;
-    slots.load(a, row, x, tl);
-    const int lane = threadIdx.x % kWave;
-    const float4 s = lane < p.parts ? p.sums[(size_t)row * p.parts + lane]
-                                    : make_float4(-FLT_MAX, 0.f, 0.f, 0.f);
-    const Row r = slots.template finish<kRest>(a, row, wave_soft({s.x, s.y}, c), tl, red);
-    if (a.loss && part == 0 && threadIdx.x == 0) a.loss[row] = r.loss;
-    if constexpr (kGrad) {
-        walk_row<T, NT, 4, true>(x, lo, hi, threadIdx.x, [&](const float (&v)[W], int at, int num) {
-            float y[W];
+    const int parts = kGrad ? p.parts : 1;
+    const uint64_t items = (uint64_t)(a.B * a.N) * parts;
+    for (uint64_t i = blockIdx.x; i < items; i += gridDim.x) {
+        const uint32_t row = item_row(i, parts, items);
+        const int part = (int)(i - (uint64_t)row * parts);
+        const uint32_t b = row / (uint32_t)a.N, n = row % (uint32_t)a.N;
+        T* grad = (T*)a.grad + (size_t)row * a.V;
+        int lo, hi;
+        part_range((int)a.V, p.parts, part, &lo, &hi);
+        if (n >= clamp_rows(a.lengths, b, a.N)) {
+            if (a.loss && part == 0 && threadIdx.x == 0) a.loss[row] = 0.f;
+            if constexpr (kGrad) write_zeros<T, NT>(grad, lo, hi);
+            continue;
+        }
+        const T* x = row_of<T>(a.logits, b, n);
+        const float c = a.scale.c, tl = kRest ? a.top_lse[row] : 0.f;
+        Slots<T, NT> slots;
+        slots.load(a, row, x, tl);
+        const int lane = threadIdx.x % kWave;
+        const float4 s = lane < p.parts ? p.sums[(size_t)row * p.parts + lane]
+                                        : make_float4(-FLT_MAX, 0.f, 0.f, 0.f);
+        const Row r = slots.template finish<kRest>(a, row, wave_soft({s.x, s.y}, c), tl, red);
+        if (a.loss && part == 0 && threadIdx.x == 0) a.loss[row] = r.loss;
+        if constexpr (kGrad) {
+            walk_row<T, NT, 4, true>(x, lo, hi, threadIdx.x, [&](const float (&v)[W], int at, int num) {
+                float y[W];
 #pragma unroll
-            for (int k = 0; k < W; ++k) y[k] = r.gain * exp2_((v[k] - r.low) * c);
-            if (num == W)
-                store_raw<T>(grad + at, pack<T>(y));
-            else
-                grad[at] = from_f<T>(y[0]);
-        });
-        slots.write(r, c, grad, lo, hi);
+                for (int k = 0; k < W; ++k) y[k] = r.gain * exp2_((v[k] - r.low) * c);
+                if (num == W)
+                    store_raw<T>(grad + at, pack<T>(y));
+                else
+                    grad[at] = from_f<T>(y[0]);
+            });
+            slots.write(r, c, grad, lo, hi);
+        }
     }
 }
 
@@ -395,7 +406,8 @@ hipError_t launch_distill(const DistillArgs& a, hipStream_t s) {
         const int V = (int)a.V;
         const DistillPlan p = distill_plan(rows, V, a.ws);
         if (p.parts > 1) {
-            const unsigned grid = (unsigned)(rows * p.parts), one = (unsigned)rows;
+            const unsigned grid = row_grid(rows * p.parts, kPartThreads);
+            const unsigned one = row_grid(rows, kPartThreads);
             // bits of a part's tokens
             const size_t lds = ((size_t)(V + p.parts - 1) / p.parts + 63) / 64 * 64 / 8;
             if (a.top_lse) {

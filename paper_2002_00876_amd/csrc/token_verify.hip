@@ -165,8 +165,7 @@ __global__ __launch_bounds__(kStatThreads) void k_verify_stats(VerifyArgs a, Pla
     const uint32_t width = 2 * (uint32_t)(t1 - t0);
     const uint64_t items = (uint64_t)p.parts * a.B * width;
     for (uint64_t i = blockIdx.x; i < items; i += gridDim.x) {
-        // (64-bit divisions take as long as a small part)
-        const uint32_t row_at = items >> 32 ? (uint32_t)(i / p.parts) : (uint32_t)i / (uint32_t)p.parts;
+        const uint32_t row_at = item_row(i, p.parts, items);
         const uint32_t part = (uint32_t)(i - (uint64_t)row_at * p.parts);
         const int64_t b = row_at / width;
         const uint32_t r = row_at % width;
@@ -276,8 +275,7 @@ __global__ __launch_bounds__(kDrawThreads) void k_verify_draw(VerifyArgs a, Plan
     const int tid = threadIdx.x;
     const uint64_t items = (uint64_t)p.draw_parts * a.B;
     for (uint64_t i = blockIdx.x; i < items; i += gridDim.x) {
-        const int64_t b = items >> 32 ? (int64_t)(i / p.draw_parts)
-                                      : (int64_t)((uint32_t)i / (uint32_t)p.draw_parts);
+        const int64_t b = item_row(i, p.draw_parts, items);
         const int part = (int)(i - (uint64_t)b * p.draw_parts);
         const int64_t n = clamp_rows(a.lengths, b, a.G);
         int32_t* out = a.out + b * (a.G + 1);

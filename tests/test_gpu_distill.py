@@ -83,6 +83,21 @@ def test_sizes(V, K, dtype, rest):
 
 
 @pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("V", [262144, 262145, 524288])
+def test_largest_vocabularies(V, rest):
+    import torch
+    from paper_2002_00876_amd import binding
+    c = _case(1, 2, V, 256, "bfloat16", V, rest=rest)
+    _check(*c, tag="largest")
+    # as many rows as are not divided for their number
+    x, t, at, l, _ = (None if y is None else y[:, :1].expand(1, 1100, *y.shape[2:]) for y in c)
+    loss = binding.distill(x, t, at, l)
+    few = binding.distill(*(None if y is None else y[:, :1] for y in c[:4]))
+    assert torch.equal(loss, loss[:, :1].expand_as(loss))
+    assert (loss[0, 0] - few[0, 0]).abs() <= R.EPS * (R.UNITS + 64) * (1 + few[0, 0].abs())
+
+
+@pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("T", [0.5, 2.0, 4.0])
 def test_temperature(T, rest):
     for dtype in TYPES:
