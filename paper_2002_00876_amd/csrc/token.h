@@ -144,6 +144,17 @@ __device__ __forceinline__ void walk_row(const T* row, int lo, int hi, int tid, 
     }
 }
 
+// The same of what nothing will read again.  Rows that start within a vector are read through the
+// caches all the same: two waves share the line between them, and it would be fetched for each
+// (statistics of 1150 rows of 100003 bfloat16: 59 us, 50 through the caches).
+template <class T, int NT, int U, class F>
+__device__ __forceinline__ void walk_once(const T* row, int lo, int hi, int tid, F f) {
+    if (reinterpret_cast<uintptr_t>(row + lo) % 16 == 0)
+        walk_row<T, NT, U, true>(row, lo, hi, tid, f);
+    else
+        walk_row<T, NT, U, false>(row, lo, hi, tid, f);
+}
+
 // Running maximum and sum of numerators.  Sums are not contracted, so that kernels which share these
 // give the same bits, however each of them is compiled.  The empty state's maximum is the lowest float, not
 // -inf, so that differences to it are never NaN.

@@ -201,10 +201,10 @@ __global__ __launch_bounds__(kStatThreads) void k_verify_stats(VerifyArgs a, Pla
         Soft s = soft_empty();
         const float c = drafted ? a.draft_scale.c : a.scale.c;
         if (drafted)
-            walk_row<TD, kStatThreads, 4, true>(y, lo, hi, threadIdx.x,
+            walk_once<TD, kStatThreads, 4>(y, lo, hi, threadIdx.x,
                                           [&](const float (&v)[kVec<TD>], int, int) { soft_push(s, v, c); });
         else
-            walk_row<TT, kStatThreads, 4, true>(x, lo, hi, threadIdx.x,
+            walk_once<TT, kStatThreads, 4>(x, lo, hi, threadIdx.x,
                                           [&](const float (&v)[kVec<TT>], int, int) { soft_push(s, v, c); });
         s = block_soft<kStatThreads>(s, c, red);
         if (threadIdx.x == 0) p.stats[row * p.parts + part] = make_float2(s.m, s.s);
