@@ -269,7 +269,7 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
 
 // One workgroup per (sequence, part of the race)
 template <class TT, class TD>
-__global__ __launch_bounds__(kDrawThreads) void k_verify_draw(VerifyArgs a, Plan p) {
+__global__ __launch_bounds__(kDrawThreads, 8) void k_verify_draw(VerifyArgs a, Plan p) {
     __shared__ Tests sh;
     __shared__ uint64_t words[kDrawThreads / kWave];
     const int tid = threadIdx.x;
