@@ -254,8 +254,10 @@ struct ChunkSoft {
     }
     __device__ __forceinline__ Soft value(float c) const {
 #pragma clang fp contract(off)
-        // 2^(v c - r) = 2^((v - m) c) 2^(m c - r)
-        return {s > 0.f ? m : -FLT_MAX, s * exp2_(-fmaf(m, c, -r))};
+        // 2^(v c - r) = 2^((v - m) c) 2^(m c - r).  A thread that has summed nothing (rows shorter than
+        // a wave's vectors, parts that end, masked stretches) still has the m it began with, whose
+        // m c - r may lie anywhere: its sum is 0, not 0 times that power.
+        return s > 0.f ? Soft{m, s * exp2_(-fmaf(m, c, -r))} : soft_empty();
     }
 };
 __device__ __forceinline__ bool far(float most) { return !(fabsf(most) <= kFar); }
