@@ -225,12 +225,17 @@ __device__ __forceinline__ float block_max(float x, float* red) {
 // The same for whole chunks of a row, at one fma, one exponential and one sum a logit: the
 // maximum is brought up to date once a chunk, and numerators are 2^(v c - r), r = m c rounded.
 // What r is rounded by is common to all numerators and goes into the sum when the pair is read
-// off (value()), so a numerator's exponent is rounded once, as a difference.  Rows whose maximum
-// lies beyond +-kFar have m c outside the floats: they are walked again, by soft_push.
-constexpr float kFar = 1e30f;
+// off (value()), so a numerator's exponent is rounded once, as a difference.  |m c| <= 2^29 keeps
+// that rounding within 32, so that numerators and their sums stay far inside the floats: a thread
+// begins at m = -k.most (|m c| = 2^29), below which tokens count for nothing beside a row's
+// maximum that is not itself beyond it.  Rows whose maximum lies beyond +-k.most (3.7e8 at T = 1)
+// are walked again, by soft_push, and what was summed here is dropped.
 struct ChunkSoft {
     float m, r, s;
-    __device__ __forceinline__ void init(float c) { m = -kFar, r = m * c, s = 0.f; }
+    __device__ __forceinline__ void init(const Scale& k) {
+#pragma clang fp contract(off)
+        m = -k.most, r = m * k.c, s = 0.f;
+    }
     __device__ __forceinline__ void raise(float most, float c) {
 #pragma clang fp contract(off)
         if (most > m) {
@@ -255,12 +260,11 @@ struct ChunkSoft {
     __device__ __forceinline__ Soft value(float c) const {
 #pragma clang fp contract(off)
         // 2^(v c - r) = 2^((v - m) c) 2^(m c - r).  A thread that has summed nothing (rows shorter than
-        // a wave's vectors, parts that end, masked stretches) still has the m it began with, whose
-        // m c - r may lie anywhere: its sum is 0, not 0 times that power.
+        // a wave's vectors, parts that end, masked stretches) is empty.
         return s > 0.f ? Soft{m, s * exp2_(-fmaf(m, c, -r))} : soft_empty();
     }
 };
-__device__ __forceinline__ bool far(float most) { return !(fabsf(most) <= kFar); }
+__device__ __forceinline__ bool far(float most, const Scale& k) { return !(fabsf(most) <= k.most); }
 
 template <int W>
 __device__ __forceinline__ float max_of(const float (&v)[W]) {

@@ -16,9 +16,11 @@ struct Rows {
 struct Scale {
     float c;       // log2(e) / T
     float inv_t;   // 1 / T
+    float most;    // logits up to here have exponents of at most 2^29
 };
 inline Scale make_scale(float t) {
-    return {(float)(1.4426950408889634 / (double)t), (float)(1.0 / (double)t)};
+    const double c = 1.4426950408889634 / (double)t;
+    return {(float)c, (float)(1.0 / (double)t), (float)(536870912.0 / c)};
 }
 
 struct TopArgs {

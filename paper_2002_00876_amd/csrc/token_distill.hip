@@ -231,7 +231,7 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs a) {
         slots.load(a, row, x, tl);
         if constexpr (kRest) slots.mark(bits, 0, V);
         ChunkSoft soft;
-        soft.init(c);
+        soft.init(a.scale);
         float most = -INFINITY;
         auto push = [&](const Raw<T>& r, int i) {
             float v[W];
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(NT) void k_distill(DistillArgs a) {
             soft.push(one, c);
         }
         Soft all = block_soft<NT>(soft.value(c), c, red);
-        if (far(block_max<NT>(most, (float*)red)))
+        if (far(block_max<NT>(most, (float*)red), a.scale))
             all = sums_again<T, NT, kRest>(x, bits, 0, V, c, red);
         const Row r = slots.template finish<kRest>(a, row, all, tl, red);
         if (a.loss && tid == 0) a.loss[row] = r.loss;
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_sums(DistillArgs a, Di
             slots.mark(bits, lo, hi);
         }
         ChunkSoft soft;
-        soft.init(c);
+        soft.init(a.scale);
         float most = -INFINITY;
         walk_row<T, NT, 4>(x, lo, hi, threadIdx.x, [&](float (&v)[W], int at, int num) {
             if constexpr (kRest) {
@@ -344,7 +344,7 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_sums(DistillArgs a, Di
         });
         Soft s = block_soft<NT>(soft.value(c), c, red);
         most = block_max<NT>(most, (float*)red);
-        if (most != -INFINITY && far(most)) s = sums_again<T, NT, kRest>(x, bits, lo, hi, c, red);
+        if (most != -INFINITY && far(most, a.scale)) s = sums_again<T, NT, kRest>(x, bits, lo, hi, c, red);
         if (threadIdx.x == 0) p.sums[i] = make_float4(s.m, s.s, most, 0.f);
         __syncthreads();   // bits are free for the next part
     }

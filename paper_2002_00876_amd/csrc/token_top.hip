@@ -415,7 +415,7 @@ __global__ __launch_bounds__(kScanThreads, 8) void k_top_scan(TopArgs a, TopPlan
     const int lo = min((int)part * per, nv), hi = min(lo + per, nv);
     const float c = a.scale.c, least = sh.least;
     ChunkSoft soft;
-    soft.init(c);
+    soft.init(a.scale);
     float most = -INFINITY;
     int found = 0;   // of this wave
     auto keep = [&](bool reaches, const Raw<T>& r, int v) {
@@ -560,7 +560,7 @@ __global__ __launch_bounds__(kTopThreads) void k_top_pick(TopArgs a, TopPlan p, 
     const int e = V / W * W + tid;   // the row's last few logits
     if (e < V && to_f(x[e]) >= least) append(to_f(x[e]), e);
     if (a.lse) {
-        if (far(most)) {
+        if (far(most, a.scale)) {
             soft = soft_empty();
             walk_row<T, NT, 1>(x, 0, V, tid,
                                [&](const float (&v)[W], int, int) { soft_push(soft, v, c); });

@@ -110,3 +110,58 @@ def test_distillation_at_any_temperature(V, B, T):
         _holes(x, teacher[1])
         for rest in (False, True) if K < V else (False,):
             _check_distill(x, teacher, T, rest, B)
+
+
+# ---- logits so large that their exponents pass 2^31 ----
+
+def _masked(x, mask, keep):
+    """Rows of x [1, 6, V] with a finite mask: everywhere, over the first half, over all but the last
+    few, at every other token, its opposite at one token and everywhere.  keep [1, 6, K]: tokens that
+    stay in the rows that are not of one value."""
+    import torch
+    V = x.shape[2]
+    hole = torch.zeros(x.shape, dtype=torch.bool, device=x.device)
+    hole[0, 1, : V // 2] = True
+    hole[0, 2, : V - 3] = True
+    hole[0, 3, ::2] = True
+    if keep is not None:
+        hole[0, 1:4].scatter_(1, keep[0, 1:4].long(), False)
+    x.masked_fill_(hole, mask)
+    x[0, 0] = mask
+    x[0, 4, V // 3] = -mask
+    x[0, 5] = -mask
+    return x
+
+
+@pytest.mark.parametrize("mask", [-1e9, -1e10, -1e12, -1e20, -1e30])
+@pytest.mark.parametrize("V,B", SHAPES)
+def test_log_sum_exp_of_finite_masks(V, B, mask):
+    for dtype, T in (("float32", 1.0), ("bfloat16", 1.0), ("float32", 0.6)):
+        _check_lse(_masked(_logits(6, V, dtype, V), mask, None), 3, T, B)
+
+
+@pytest.mark.parametrize("V,B", SHAPES)
+def test_log_sum_exp_at_the_least_temperature(V, B):
+    # logits of some thousands have exponents of 10^9 here
+    _check_lse(_logits(4, V, "float32", V) * 2 + 3000, 3, 1e-6, B)
+    _check_lse(_logits(4, V, "float16", V) * 2 - 3000, 3, 1e-6, B)
+
+
+@pytest.mark.parametrize("mask", [-1e9, -1e10, -1e12, -1e20, -1e30])
+@pytest.mark.parametrize("V,B", SHAPES)
+def test_distillation_of_finite_masks(V, B, mask):
+    for dtype, T in (("float32", 1.0), ("bfloat16", 1.0), ("float32", 0.6)):
+        x = _logits(6, V, dtype, V)
+        teacher = _teacher(x, 5, T, V)
+        x = _masked(x, mask, teacher[1])
+        for rest in (False, True):
+            # (in float64 a sum over masks of 10^20 would lose its logarithm beside unmasked slots:
+            # every row here has other tokens outside the slots, or one value throughout)
+            _check_distill(x, teacher, T, rest, B)
+
+
+@pytest.mark.parametrize("V,B", SHAPES)
+def test_distillation_of_far_logits_at_a_low_temperature(V, B):
+    x = _logits(3, V, "float32", V)
+    teacher = _teacher(x, 5, 1e-3, V)
+    _check_distill(x + 4e6, teacher, 1e-3, False, B)
