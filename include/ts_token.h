@@ -84,7 +84,8 @@ ts_status ts_token_top(const void* logits, int dtype, int64_t stride_b, int64_t 
  * exp(t_k / T - top_lse), and what the slots leave, p_r = 1 - sum_k p_k, is one class of its
  * own that the student gives q_r, its probability outside the slots:
  *   loss = sum_k p_k (log p_k - log q[i_k]) + p_r (log p_r - log q_r).
- * p_r below 2^-20 counts as 0: that is the rounding of 32-bit sums.
+ * p_r below 2^-22 (8 + |top_lse|) counts as 0: that is the rounding of the p_k and of top_lse in 32
+ * bits.  It is 0 too where the slots hold every token of the vocabulary.
  *   loss     float32 [B, N]: +inf where q is 0 and p is not; 0 for padding and for rows with no
  *            teacher probability at all.
  */

@@ -26,7 +26,12 @@
 namespace tsc {
 namespace {
 
-constexpr float kMinRest = 9.5367431640625e-7f;   // 2^-20
+// What the slots leave, 1 - sum p with p_k = exp(t_k / T - lse), is known to about 2^-23 (|lse| + 8):
+// t_k / T and lse are each rounded by 2^-24 of themselves and t_k / T = lse + log p_k, of which the p
+// take |lse| + log K on the average; the 8 stands for that, exp and the sum.  Less than twice this is
+// no rest: where the student gives nothing outside the slots, its loss would be infinite.
+constexpr float kMinRest = 2.38418579e-7f;   // 2^-22
+__device__ __forceinline__ float min_rest(float lse) { return kMinRest * (8.f + fabsf(lse)); }
 constexpr int kPartThreads = 256;
 constexpr int kWantParts = 1024;   // workgroups that fill the chip
 constexpr int kMinPart = 4096;     // tokens of a part
@@ -133,7 +138,13 @@ struct Slots {
         float keep = mass > 0.f ? 1.f : 0.f;
         if constexpr (kRest) {
             float rest = 1.f - mass;
-            if (!(rest > kMinRest)) rest = 0.f;
+            if (tl != -INFINITY && !(rest > min_rest(tl))) rest = 0.f;
+            if (a.K == (int)a.V) {   // (and where no token is outside the slots)
+                float filled = 0.f;
+#pragma unroll
+                for (int q = 0; q < kSlots<NT>; ++q) filled += slot[q].at >= 0 ? 1.f : 0.f;
+                if (block_sum<NT>(filled, redf) == (float)a.K) rest = 0.f;
+            }
             const float low =
                 soft.s > 0.f ? (soft.m - all.m) * inv_t + logf(soft.s) - ls : -INFINITY;
             if (rest > 0.f) kl += rest * (logf(rest) - low);

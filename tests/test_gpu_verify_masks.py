@@ -1,0 +1,34 @@
+"""Verification of drafts whose logits are masked, by -inf or by the type's lowest value, on either
+side, or whose probabilities are below the 32-bit floats; against float64."""
+import pytest
+
+import token_ref as R
+from test_gpu_verify import _case, _check
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+
+
+def _sums(d, dT):
+    import torch
+    return torch.logsumexp(d.double() / dT, 2).float()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T", [1.0, 0.7, 2.0])
+@pytest.mark.parametrize("V", [50, 20000])
+def test_masked_drafts(V, T, dtype):
+    import torch
+    x, d, z, u, noise = _case(6, 2, V, dtype, 20 + V, T=T, dT=T)
+    lowest = torch.finfo(x.dtype).min
+    at = z[:, 0].long()
+    for b, (p, q) in enumerate([(None, lowest), (None, -INF), (lowest, lowest), (lowest, -INF),
+                                (-INF, lowest), (-INF, -INF)]):
+        # q = 0: accepted where p > 0, whatever the uniform, and refused where p = 0
+        if p is not None:
+            x[b, 0, at[b]] = p
+        d[b, 0, at[b]] = q
+    u[:, 0] = 1 - 2.0 ** -24
+    _check(x, d, z, u, noise, T=T, dT=T, tag="masked drafts")
+    _check(x, d, z, u, noise, dl=_sums(d, T), T=T, dT=T, tag="masked drafts, their sums")
