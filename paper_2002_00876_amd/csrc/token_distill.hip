@@ -138,7 +138,7 @@ struct Slots {
         float keep = mass > 0.f ? 1.f : 0.f;
         if constexpr (kRest) {
             float rest = 1.f - mass;
-            if (tl != -INFINITY && !(rest > min_rest(tl))) rest = 0.f;
+            if (!(rest > min_rest(tl))) rest = 0.f;
             if (a.K == (int)a.V) {   // (and where no token is outside the slots)
                 float filled = 0.f;
 #pragma unroll
@@ -149,6 +149,7 @@ struct Slots {
                 soft.s > 0.f ? (soft.m - all.m) * inv_t + logf(soft.s) - ls : -INFINITY;
             if (rest > 0.f) kl += rest * (logf(rest) - low);
             keep = exp_(low) - rest;
+            if (tl == -INFINITY) kl = keep = 0.f;   // no teacher, whatever the student's row
         }
         Row r;
         r.loss = kl;

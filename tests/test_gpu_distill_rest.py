@@ -135,3 +135,22 @@ def test_a_rest_that_is_there(V, lse):
         low[0, 0] = -INF
         low[0, 0].scatter_(0, i[0, 0], student[0, 0].gather(0, i[0, 0]))
         _check(low, v, i.int(), l, T, f"rest {left}, lse {lse}")
+
+
+@pytest.mark.parametrize("V,repeat", [(1, 1), (30, 1), (2000, 1), (9000, 1), (2000, 600), (30011, 300)])
+def test_neither_side_says_anything(V, repeat):
+    # a teacher's row without a finite logit has no probability to compare with: loss and gradient
+    # are 0, whatever the student's row is
+    import torch
+    teacher, student = _rows(1, 4, V, "float32", V, 0, 1.0)
+    K = min(V, 5)
+    v, i = teacher.topk(K, 2)
+    l = torch.logsumexp(v, 2) + 0.1
+    v[0, :3] = -INF
+    l[0, :3] = -INF
+    student[0, 0] = -INF
+    student[0, 1] = torch.finfo(torch.float32).min
+    _check(student, v, i.int(), l, 1.0, "nothing", repeat)
+    from paper_2002_00876_amd import binding
+    loss, grad = binding.distill_grad(student, v, i.int(), l)
+    assert not loss[0, :3].any() and not grad[0, :3].any()
