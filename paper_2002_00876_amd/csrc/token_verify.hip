@@ -95,10 +95,11 @@ __device__ __forceinline__ float log_prob(float x, Soft s, const Scale& k) {
 }
 
 // 2^((x - m) c) with the product's rounding made good: the hardware's exponential (2^-23) is
-// what is left of the error, also far below the maximum
+// what is left of the error, also far below the maximum.  0 from an exponent of -200 on, where the
+// product may be infinite (tokens masked with the type's lowest value) and nothing can be made good.
 __device__ __forceinline__ float numerator(float x, float m, float c) {
     const float d = x - m, e = d * c;
-    return exp2_(e) * fmaf(fmaf(d, c, -e), 0.69314718f, 1.f);
+    return e > -200.f ? exp2_(e) * fmaf(fmaf(d, c, -e), 0.69314718f, 1.f) : 0.f;
 }
 
 // Whether a draft of target's logit x and draft's y is accepted, and its log-probability.
@@ -108,11 +109,11 @@ __device__ __forceinline__ bool accepts(const VerifyArgs& a, float x, float y, f
     *logp = 0.f;
     if (!(x > -INFINITY)) return false;
     *logp = log_prob(x, sp, a.scale);
+    const float c = a.scale.c, cq = a.draft_scale.c;
     if (y == -INFINITY) return true;
-    const float c = a.draft_scale.c;
-    const double q = a.draft_lse ? numerator(y, lse / a.draft_scale.inv_t, c) : numerator(y, sq.m, c);
-    return (double)u * q * (double)sp.s <
-           (double)numerator(x, sp.m, a.scale.c) * (a.draft_lse ? 1.0 : (double)sq.s);
+    const float mq = a.draft_lse ? lse / a.draft_scale.inv_t : sq.m;
+    return (double)u * numerator(y, mq, cq) * (double)sp.s <
+           (double)numerator(x, sp.m, c) * (a.draft_lse ? 1.0 : (double)sq.s);
 }
 
 struct Tests {
