@@ -103,13 +103,15 @@ __device__ __forceinline__ float numerator(float x, float m, float c) {
 }
 
 // Whether a draft of target's logit x and draft's y is accepted, and its log-probability.
-// u q < p without a division: u e_q s_p < e_p s_q, the products in 64 bits.
+// u q < p without a division: u e_q s_p < e_p s_q, the products in 64 bits.  A p below the
+// 64-bit floats (2^-1074) is 0, and refuses, as -inf does.
 __device__ __forceinline__ bool accepts(const VerifyArgs& a, float x, float y, float u, float lse,
                                         Soft sp, Soft sq, float* logp) {
     *logp = 0.f;
     if (!(x > -INFINITY)) return false;
     *logp = log_prob(x, sp, a.scale);
     const float c = a.scale.c, cq = a.draft_scale.c;
+    if (!((x - sp.m) * c > -1074.f)) return false;
     if (y == -INFINITY) return true;
     const float mq = a.draft_lse ? lse / a.draft_scale.inv_t : sq.m;
     return (double)u * numerator(y, mq, cq) * (double)sp.s <

@@ -32,3 +32,19 @@ def test_masked_drafts(V, T, dtype):
     u[:, 0] = 1 - 2.0 ** -24
     _check(x, d, z, u, noise, T=T, dT=T, tag="masked drafts")
     _check(x, d, z, u, noise, dl=_sums(d, T), T=T, dT=T, tag="masked drafts, their sums")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T", [1.0, 0.7, 2.0])
+@pytest.mark.parametrize("V", [50, 20000])
+def test_drafts_masked_on_both_sides_in_different_ways(V, T, dtype):
+    # p of the type's lowest value is 0 in 64 bits too: it refuses a draft of q = 0
+    import torch
+    x, d, z, u, noise = _case(2, 2, V, dtype, 50 + V, T=T, dT=T)
+    at = z[:, 0].long()
+    x[0, 0, at[0]] = torch.finfo(x.dtype).min
+    d[0, 0, at[0]] = -INF
+    x[1, 0, at[1]] = x[1, 0].max() - 600 * T             # e^-600 is not, and does not
+    d[1, 0, at[1]] = -INF
+    _check(x, d, z, u, noise, T=T, dT=T, tag="masked twice")
+    _check(x, d, z, u, noise, dl=_sums(d, T), T=T, dT=T, tag="masked twice, their sums")
