@@ -94,28 +94,30 @@ __device__ __forceinline__ float log_prob(float x, Soft s, const Scale& k) {
     return (x - s.m) * k.inv_t - logf(s.s);
 }
 
-// 2^((x - m) c) with the product's rounding made good: the hardware's exponential (2^-23) is
+// 2^((x - m) c - k), with the product's rounding made good: the hardware's exponential (2^-23) is
 // what is left of the error, also far below the maximum.  0 from an exponent of -200 on, where the
 // product may be infinite (tokens masked with the type's lowest value) and nothing can be made good.
-__device__ __forceinline__ float numerator(float x, float m, float c) {
+__device__ __forceinline__ float numerator(float x, float m, float c, float k) {
     const float d = x - m, e = d * c;
-    return e > -200.f ? exp2_(e) * fmaf(fmaf(d, c, -e), 0.69314718f, 1.f) : 0.f;
+    return e - k > -200.f ? exp2_(e - k) * fmaf(fmaf(d, c, -e), 0.69314718f, 1.f) : 0.f;
 }
 
 // Whether a draft of target's logit x and draft's y is accepted, and its log-probability.
-// u q < p without a division: u e_q s_p < e_p s_q, the products in 64 bits.  A p below the
+// u q < p without a division: u e_q s_p < e_p s_q, the products in 64 bits.  Where both numerators
+// are far below the 32-bit floats, both exponents are taken from the larger one's.  A p below the
 // 64-bit floats (2^-1074) is 0, and refuses, as -inf does.
 __device__ __forceinline__ bool accepts(const VerifyArgs& a, float x, float y, float u, float lse,
                                         Soft sp, Soft sq, float* logp) {
     *logp = 0.f;
     if (!(x > -INFINITY)) return false;
     *logp = log_prob(x, sp, a.scale);
-    const float c = a.scale.c, cq = a.draft_scale.c;
-    if (!((x - sp.m) * c > -1074.f)) return false;
+    const float c = a.scale.c, cq = a.draft_scale.c, ep = (x - sp.m) * c;
+    if (!(ep > -1074.f)) return false;
     if (y == -INFINITY) return true;
     const float mq = a.draft_lse ? lse / a.draft_scale.inv_t : sq.m;
-    return (double)u * numerator(y, mq, cq) * (double)sp.s <
-           (double)numerator(x, sp.m, c) * (a.draft_lse ? 1.0 : (double)sq.s);
+    const float k = fminf(fmaxf(ep, (y - mq) * cq) + 100.f, 0.f);
+    return (double)u * numerator(y, mq, cq, k) * (double)sp.s <
+           (double)numerator(x, sp.m, c, k) * (a.draft_lse ? 1.0 : (double)sq.s);
 }
 
 struct Tests {

@@ -48,3 +48,15 @@ def test_drafts_masked_on_both_sides_in_different_ways(V, T, dtype):
     d[1, 0, at[1]] = -INF
     _check(x, d, z, u, noise, T=T, dT=T, tag="masked twice")
     _check(x, d, z, u, noise, dl=_sums(d, T), T=T, dT=T, tag="masked twice, their sums")
+
+
+@pytest.mark.parametrize("V", [50, 20000])
+def test_drafts_far_below_the_maximum(V):
+    # p and q of e^-200 and e^-300: neither is a 32-bit float, which is larger is decided all the same
+    x, d, z, u, noise = _case(4, 2, V, "float32", 40 + V)
+    at = z[:, 0].long()
+    for b, (p, q) in enumerate([(200, 300), (300, 200), (95, 200), (200, 95)]):
+        x[b, 0, at[b]] = x[b, 0].max() - p
+        d[b, 0, at[b]] = d[b, 0].max() - q
+    _check(x, d, z, u, noise, tag="far drafts")
+    _check(x, d, z, u, noise, dl=_sums(d, 1.0), tag="far drafts, their sums")
