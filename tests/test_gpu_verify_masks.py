@@ -60,3 +60,16 @@ def test_drafts_far_below_the_maximum(V):
         d[b, 0, at[b]] = d[b, 0].max() - q
     _check(x, d, z, u, noise, tag="far drafts")
     _check(x, d, z, u, noise, dl=_sums(d, 1.0), tag="far drafts, their sums")
+
+
+@pytest.mark.parametrize("V", [50, 20000])
+def test_drafts_from_nowhere_with_their_sums(V):
+    # a draft's row without a finite logit has a log-sum-exp of -inf and q = 0: what remains of a
+    # refused draft is the target's row
+    x, d, z, u, noise = _case(5, 2, V, "float32", 30 + V)
+    d[:, 0] = -INF
+    x[1, 0, z[1, 0].long()] = -INF
+    x[2, 0] = -INF
+    z[3, 0] = -1
+    _check(x, d, z, u, noise, tag="nowhere")
+    _check(x, d, z, u, noise, dl=_sums(d, 1.0), tag="nowhere, its sums")
