@@ -92,9 +92,10 @@ __device__ uint32_t threshold(const uint32_t (&key)[J], int K, uint32_t lo, uint
     return lo;
 }
 
-// The list's words each find their place among them
+// The list's words, of logits x, each find their place among them
 template <class T, int NT, class S>
-__device__ __forceinline__ void write_places(const TopArgs& a, uint32_t row, int n, const S& sh) {
+__device__ __forceinline__ void write_places(const TopArgs& a, const T* x, uint32_t row, int n,
+                                             const S& sh) {
     T* values = (T*)a.values + (size_t)row * a.K;
     int32_t* indices = a.indices + (size_t)row * a.K;
     for (int i = threadIdx.x; i < n; i += NT) {
@@ -105,8 +106,10 @@ __device__ __forceinline__ void write_places(const TopArgs& a, uint32_t row, int
             for (int k = 0; k < 4; ++k) place += sh.list[j + k] > w;
         for (; j < n; ++j) place += sh.list[j] > w;
         if (place < a.K) {
-            values[place] = from_f<T>(of_key((uint32_t)(w >> 32)));
-            indices[place] = (int32_t)~(uint32_t)w;
+            const int at = (int)~(uint32_t)w;
+            const float v = of_key((uint32_t)(w >> 32));
+            values[place] = v == 0.f ? x[at] : from_f<T>(v);   // a key does not know a zero's sign
+            indices[place] = at;
         }
     }
 }
@@ -200,7 +203,7 @@ __global__ __launch_bounds__(kWave) void k_top_short(TopArgs a) {
                 have = append_ordered<NT>(kj == lo, word_of(lo, j * NT + tid), have, K, sh);
             }
         __syncthreads();
-        write_places<T, NT>(a, row, have, sh);
+        write_places<T, NT>(a, x, row, have, sh);
         __syncthreads();   // the list is free for the next row
     }
 }
@@ -595,7 +598,7 @@ __global__ __launch_bounds__(kTopThreads) void k_top_pick(TopArgs a, TopPlan p, 
     // -inf is none of the K largest before every finite logit is
     if (have < K) have = append_equal<T, NT>(x, V, K, key_of(-INFINITY), have, sh);
     __syncthreads();
-    write_places<T, NT>(a, row, have, sh);
+    write_places<T, NT>(a, x, row, have, sh);
 }
 
 }  // namespace
