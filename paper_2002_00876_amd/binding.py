@@ -356,6 +356,8 @@ def token_workspace_bytes(op, B, N, V, K=1):
 
 def _token_workspace(op, B, N, V, K, device, ws):
     if ws is not None:
+        if ws.device != device or not ws.is_contiguous():
+            raise ValueError("ws must be a contiguous tensor on the same device as the logits")
         return ws, ws.numel() * ws.element_size()
     need = token_workspace_bytes(op, B, N, V, K)
     if need == 0:
