@@ -113,7 +113,7 @@ __device__ __forceinline__ bool accepts(const VerifyArgs& a, float x, float y, f
     *logp = log_prob(x, sp, a.scale);
     const float c = a.scale.c, cq = a.draft_scale.c, ep = (x - sp.m) * c;
     if (!(ep > -1074.f)) return false;
-    if (y == -INFINITY) return true;
+    if (y == -INFINITY || (a.draft_lse && lse == -INFINITY)) return true;
     const float mq = a.draft_lse ? lse / a.draft_scale.inv_t : sq.m;
     const float k = fminf(fmaxf(ep, (y - mq) * cq) + 100.f, 0.f);
     return (double)u * numerator(y, mq, cq, k) * (double)sp.s <

@@ -73,3 +73,17 @@ def test_drafts_from_nowhere_with_their_sums(V):
     z[3, 0] = -1
     _check(x, d, z, u, noise, tag="nowhere")
     _check(x, d, z, u, noise, dl=_sums(d, 1.0), tag="nowhere, its sums")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("V", [1, 50, 20000])
+def test_drafts_whose_sums_underflow(V, dtype):
+    # a draft's row of the type's lowest value has a log-sum-exp below the floats at T < 1: given as
+    # -inf it says q = 0
+    import torch
+    x, d, z, u, noise = _case(3, 2, V, dtype, 60 + V, T=0.5, dT=0.5)
+    d[:, 0] = torch.finfo(d.dtype).min
+    x[1, 0, z[1, 0].long()] = -INF
+    sums = _sums(d, 0.5)
+    assert bool((sums[:, 0] == -INF).all())
+    _check(x, d, z, u, noise, dl=sums, T=0.5, dT=0.5, tag="sums of -inf")
