@@ -245,9 +245,9 @@ __device__ __forceinline__ Race race_of(const VerifyArgs& a, int64_t b, int64_t 
                                         Soft sp, Soft sq) {
     Race r{sp.m, sp.s > 0.f ? 1.f / sp.s : 0.f, a.scale.c, 0.f, 0.f, a.draft_scale.c, refused};
     if (refused && a.draft_lse) {
-        // (a row without a finite logit, of log-sum-exp -inf, has q = 0: no difference of infinities)
+        // (a log-sum-exp of -inf says q = 0: no difference of infinities, no power above the floats)
         const float lse = a.draft_lse[b * a.G + at];
-        r.mq = lse > -INFINITY ? lse / a.draft_scale.inv_t : 0.f;
+        r.mq = lse > -INFINITY ? lse / a.draft_scale.inv_t : FLT_MAX;
         r.iq = lse > -INFINITY ? 1.f : 0.f;
     } else if (refused) {
         r.mq = sq.m;

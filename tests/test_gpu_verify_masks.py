@@ -87,3 +87,16 @@ def test_drafts_whose_sums_underflow(V, dtype):
     sums = _sums(d, 0.5)
     assert bool((sums[:, 0] == -INF).all())
     _check(x, d, z, u, noise, dl=sums, T=0.5, dT=0.5, tag="sums of -inf")
+
+
+@pytest.mark.parametrize("V", [50, 20000])
+def test_sums_of_nothing_beside_large_logits(V):
+    # q = 0 is what a log-sum-exp of -inf says, whatever the draft's logits: a refused draft leaves p
+    import torch
+    x, d, z, u, noise = _case(4, 2, V, "float32", 70 + V)
+    d[:, 0, ::2] += 300
+    sums = _sums(d, 1.0)
+    sums[:, 0] = -INF
+    x[:, 0] = torch.where(x[:, 0] == x[:, 0].amax(1, keepdim=True), 2.0, x[:, 0].clamp(max=2.0))
+    z[:2, 0] = -1
+    _check(x, d, z, u, noise, dl=sums, tag="sums of nothing")
