@@ -123,15 +123,18 @@ ts_status ts_token_distill_grad(const void* logits, int dtype, int64_t stride_b,
  *   draft    [B, G, V] logits that the drafts were drawn from, q_t, at draft_temperature (a
  *            chain's rows of log-probabilities are such logits).  May be NULL only when G == 0.
  *   draft_lse float32 [B, G] or NULL: log sum_v exp(draft_v / draft_temperature), where the
- *            caller has it (0 for normalised rows); it saves the sum over the drafts' rows.
- *   tokens   int32 [B, G]: the drafts z_t.  One outside [0, V) is never accepted.
+ *            caller has it (0 for normalised rows); it saves the sum over the drafts' rows.  -inf:
+ *            q_t is 0 throughout.
+ *   tokens   int32 [B, G]: the drafts z_t.  One outside [0, V) is never accepted; TS_CHECK=1 returns
+ *            TS_ERR_LABELS for one among a sequence's lengths[b] drafts.
  *   uniforms float32 [B, G] in [0, 1), noise float32 [B, V], positive, independent standard
  *            exponentials: the caller's random numbers.
  *   lengths  int32 [B] or NULL: drafts of each sequence, 0 <= lengths[b] <= G.
  *   G        >= 0, B * (G + 1) <= 2^29.
- * Draft t is accepted when all before it are and uniforms_t * q_t(z_t) < p_t(z_t).  After a
- * accepted drafts one more token is drawn: from max(p_a - q_a, 0), normalised, where draft a
- * was refused, and from p_a where there was none (or where max(p_a - q_a, 0) is 0 throughout).
+ * Draft t is accepted when all before it are and uniforms_t * q_t(z_t) < p_t(z_t); a p below
+ * 2^-1074 of its row's largest counts as 0.  After a accepted drafts one more token is drawn: from
+ * max(p_a - q_a, 0), normalised, where draft a was refused, and from p_a where there was none (or
+ * where max(p_a - q_a, 0) is 0 throughout).
  * The draw is argmax_v r_v / noise_v, the lowest index of equal ones: the first of
  * exponential clocks of rates r_v rings at v with probability r_v / sum r.  It needs no sum
  * of r and its outcome does not depend on how a row is divided.  A target's row without a

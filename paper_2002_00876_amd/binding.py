@@ -411,7 +411,7 @@ def distill(logits, top_values, top_indices, top_lse=None, lengths=None, tempera
     [B, N, V], from a teacher's top logits: values [B, N, K] at indices int32 [B, N, K] (an index
     outside the vocabulary is an empty slot).  Without top_lse the teacher is normalised over
     its slots; with it (its log-sum-exp [B, N] at this temperature) what they leave is one class.
-    0 for padding."""
+    0 for padding.  The loss has no graph: distill_grad() is its backward pass."""
     head, kept, (B, N, V, K), dev = _prep_teacher(logits, top_values, top_indices, top_lse, lengths)
     if out is None:
         loss = torch.empty((B, N), dtype=torch.float32, device=dev)
