@@ -13,8 +13,9 @@
 // walked over, so one walk over the row gives its sums and a second one writes the gradient,
 // after which the K slots' values are written over it.
 //
-// The loss is bound by its read (3072 rows of 32000 float32 58 us, 6.8 TB/s), the gradient by what
-// crosses the fabric: two reads and a write (8192 rows of 131072 bfloat16 900 us, 7.1 TB/s).
+// The loss is bound by its read (3072 rows of 32000 float32 58 to 62 us, 6.4 to 6.8 TB/s), the
+// gradient by what crosses the fabric: two reads and a write (8192 rows of 131072 bfloat16 900 us,
+// 7.1 TB/s).
 //
 // One workgroup takes a row (k_distill).  For the gradient it reads it again backwards: what was
 // read last is still in the L2, the rest in the memory-side cache.  Where the rows are few each is

@@ -292,7 +292,10 @@ constexpr int kKeep = 252;        // vectors that a wave keeps: 8 workgroups fil
 constexpr int kScanWaves = kScanThreads / kWave;
 constexpr int kScanWant = 2048;   // workgroups that fill the chip
 constexpr int kMinScan = 2048;    // elements of a part
-constexpr int64_t kSlab = 4096;   // parts of rows that the workspace holds at once
+// Parts of rows that the workspace holds at once, at 20 KB each (83 MB).  Larger calls take a pair of
+// launches for each slab: 16384 rows of 8000 bfloat16 165 us, and 142 by 8192, 131 by 16384 parts; the
+// workspace is what bounds it, and up to 4096 rows it makes no difference.
+constexpr int64_t kSlab = 4096;
 
 struct TopPlan {
     int parts;

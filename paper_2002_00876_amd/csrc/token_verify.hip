@@ -11,7 +11,7 @@
 // are a few numbers a draft.
 //
 // Both are bound by reading: 8 drafts of 256 sequences over 131072 bfloat16 tokens take 187 us, 1.2 GB
-// at 6.4 TB/s, of which refused drafts save what follows them; of 1 sequence 4.6 and 6.9 us, a few
+// at 6.4 TB/s, of which refused drafts save what follows them; of 1 sequence about 5 and 7 us, a few
 // dependent loads and two atomics across the chip.
 #include <hip/hip_runtime.h>
 
@@ -39,7 +39,7 @@ constexpr int kStatParts = 2048, kDrawParts = 1024;   // workgroups that fill th
 
 // Parts of a row: enough workgroups to fill the chip where the rows are few, and none so long that
 // the chip waits for the last of them where sequences have unequal numbers of drafts (128
-// sequences of up to 8 over 100003 tokens: 97 us in whole rows, 88 in quarters)
+// sequences of up to 8 over 100003 tokens: both kernels take 83 us in whole rows, 75 in quarters)
 inline int parts_of(int64_t rows, int64_t V, int64_t want) {
     int64_t p = (want + rows - 1) / rows;
     if (p < (V + kMaxPart - 1) / kMaxPart) p = (V + kMaxPart - 1) / kMaxPart;
@@ -274,7 +274,11 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t x) {
     return x;
 }
 
-// One workgroup per (sequence, part of the race)
+// One workgroup per (sequence, part of the race).  Eight waves a SIMD are asked for: of the 80 VGPRs
+// that it would take (5 to 6 waves) 64 are left and 3 or 4 go to scratch, outside the race's loop.
+// What it gains where rows are many it loses in part where they are few (us for both kernels, without /
+// with: 128 sequences of 8 drafts over 100003 bfloat16 77 / 75, over 100096 76.6 / 74.2, over 50000
+// float32 69.3 / 68.7; 1 of 5 over 131072 bfloat16 11.7 / 12.2, float32 12.7 / 13.3; 8 of 5 23.4 / 24.3).
 template <class TT, class TD>
 __global__ __launch_bounds__(kDrawThreads, 8) void k_verify_draw(VerifyArgs a, Plan p) {
     __shared__ Tests sh;
