@@ -1,7 +1,8 @@
 """Python binding of libtschain.so: marshals torch tensors (device memory and the
-current HIP stream) into the C ABI of include/ts_chain.h and include/ts_token.h.  No arithmetic happens here;
-every step runs in the library's HIP kernels.  If the library is missing, every call
-raises: there is no fallback."""
+current HIP stream) into the C ABI of include/ts_chain.h, include/ts_token.h and
+include/ts_cache.h.  No arithmetic happens here; every step runs in the library's HIP kernels.  If
+the library is missing, every call raises: there is no fallback."""
+import contextlib
 import ctypes
 import os
 
@@ -19,6 +20,12 @@ STATUS = {0: "TS_OK", -1: "TS_ERR_NULL_ARG", -2: "TS_ERR_BAD_DIM", -3: "TS_ERR_W
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 _lib = None
+
+
+class CacheLayout(ctypes.Structure):
+    """ts_cache_layout: sizes of a paged cache and its strides in elements."""
+    _fields_ = [(n, ctypes.c_int64) for n in ("pages", "page_size", "heads", "head_size",
+                                              "stride_page", "stride_token", "stride_head")]
 
 
 class TsError(RuntimeError):
@@ -65,7 +72,16 @@ def lib():
                                             f32, p, p, p, sz, p]
         L.ts_token_verify.argtypes = [p, ci, i64, i64, p, ci, i64, i64, p, p, p, p, p, i64, i64,
                                       i64, f32, f32, p, p, p, p, sz, p]
-        for f in ("ts_token_top", "ts_token_distill", "ts_token_distill_grad", "ts_token_verify",
+        strides, layout = ctypes.POINTER(i64), ctypes.POINTER(CacheLayout)
+        L.ts_cache_max_head.restype = ci
+        L.ts_cache_max_nodes.restype = ci
+        L.ts_cache_append.argtypes = [p, p, p, strides, ci, p, i64, ci, p, p, p, layout, p, i64, p,
+                                      p, i64, i64, i64, p, p]
+        L.ts_cache_attend_workspace_bytes.argtypes = [i64] * 5
+        L.ts_cache_attend_workspace_bytes.restype = sz
+        L.ts_cache_attend.argtypes = [p, strides, ci, p, p, layout, p, i64, p, p, p, i64, i64, i64,
+                                      f32, p, p, p, sz, p]
+        for f in ("ts_cache_append", "ts_cache_attend", "ts_token_top", "ts_token_distill", "ts_token_distill_grad", "ts_token_verify",
                   "ts_chain_logpartition", "ts_chain_marginals", "ts_chain_viterbi",
                   "ts_chain_marginals_noalloc",
                   "ts_chain_marginals_viterbi", "ts_chain_entropy", "ts_chain_log_density",
@@ -91,6 +107,13 @@ def _stream(device):
     # the current stream's handle without a Stream object around it (0.2 instead of 2.0 us, of
     # the 9 us that a smallest call takes on the host)
     return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _device(device):
+    """Makes a tensor's device the current one for a call, where it is not."""
+    if torch._C._cuda_getDevice() == device.index:
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
 
 
 def _prep(pot, lengths):
@@ -477,3 +500,124 @@ def verify(target, draft, tokens, uniforms, noise, lengths=None, draft_lse=None,
                                  _ptr(emitted), _ptr(accepted), _ptr(logp), _ptr(w), nb,
                                  _stream(dev)))
     return emitted, accepted, logp
+
+
+# ---- a larger model's paged cache of keys and values (include/ts_cache.h) ----
+
+_Strides = {n: ctypes.c_int64 * n for n in (3, 9)}
+
+
+def _prep_heads(x, name, dtype=None, shape=None, device=None):
+    """x [B, N, H, D] with heads that start at multiples of 16 bytes (copied only where they do
+    not) and contiguous elements, and its strides."""
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if x.dim() != 4 or x.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"{name} must be bfloat16 or float16 [B, N, H, D]")
+    if (dtype, shape, device) != (None, None, None) and (
+            x.dtype != dtype or tuple(x.shape) != shape or x.device != device):
+        raise ValueError(f"{name} must be {dtype} {list(shape)} on {device}")
+    sb, sn, sh, sd = x.stride()
+    if sd != 1 or sb % 8 or sn % 8 or sh % 8 or x.data_ptr() % 16:
+        # (a size of 1 may have any stride: a copy gives it an ordinary one)
+        x = x.clone(memory_format=torch.contiguous_format)
+        sb, sn, sh, sd = x.stride()
+    return x, (sb, sn, sh)
+
+
+def _prep_cache(k_cache, v_cache, pages, starts, lengths, B, dtype, device):
+    for x, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        if x.dim() != 4 or x.dtype != dtype or x.device != device:
+            raise ValueError(f"{name} must be {dtype} [P, S, Hk, D] on {device}")
+    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
+        raise ValueError("k_cache and v_cache must have the same shape and strides")
+    if k_cache.shape[3] > 1 and k_cache.stride(3) != 1:
+        raise ValueError("the elements of a head of the caches must be contiguous")
+    if pages.dim() != 2:
+        raise ValueError("pages must be int32 [B, M]")
+    pages = _prep_small(pages, "pages", torch.int32, (B, pages.shape[1]), device)
+    starts = _prep_small(starts, "starts", torch.int32, (B,), device)
+    lengths = _prep_small(lengths, "lengths", torch.int32, (B,), device)
+    return CacheLayout(*k_cache.shape, *k_cache.stride()[:3]), pages, starts, lengths
+
+
+def cache_append(k, v, k_cache, v_cache, pages, starts, lengths=None, q=None, freqs=None,
+                 positions=None, neighbours=False, out=None):
+    """Appends keys and values k, v [B, N, Hk, D] to the paged caches [P, S, Hk, D], in place: token n
+    of a sequence goes to slot starts[b] + n (int32 [B]), slot j lies in page pages[b, j // S]
+    (int32 [B, M]) at j % S.  With freqs (float32 [R / 2]: angle per position) the first R elements
+    of the heads of k, and of q [B, N, Hq, D] where it is given, are rotated by the token's
+    position: its slot, or positions (int32 [B, N]); pairs are (i, i + R / 2), or (2 i, 2 i + 1) with
+    neighbours.  Tokens from lengths (int32 [B]) on are padding.  Returns the rotated q (zeros for
+    padding; `out`, which may be q itself, where it is given), or None.  bfloat16 or float16, D a
+    multiple of 8 up to 256."""
+    k, ks = _prep_heads(k, "k")
+    B, N, Hk, D = k.shape
+    dtype, dev = k.dtype, k.device
+    v, vs = _prep_heads(v, "v", dtype, (B, N, Hk, D), dev)
+    layout, pages, starts, lengths = _prep_cache(k_cache, v_cache, pages, starts, lengths, B, dtype,
+                                                 dev)
+    if k_cache.shape[2:] != (Hk, D):
+        raise ValueError(f"the caches must be [P, S, {Hk}, {D}]")
+    positions = _prep_small(positions, "positions", torch.int32, (B, N), dev)
+    R = 0
+    if freqs is not None:
+        R = 2 * freqs.numel()
+        freqs = _prep_small(freqs, "freqs", torch.float32, (R // 2,), dev)
+    Hq, qs = 0, (0, 0, 0)
+    if q is not None:
+        Hq = q.shape[2] if q.dim() == 4 else 0
+        q, qs = _prep_heads(q, "q", dtype, (B, N, Hq, D), dev)
+        if out is None:
+            out = torch.empty((B, N, Hq, D), dtype=dtype, device=dev)
+        else:
+            _check_outs((out,), ("out",), (dtype,), ((B, N, Hq, D),), dev)
+    elif out is not None:
+        raise ValueError("out is q's: it needs q")
+    with _device(dev):
+        _check(lib().ts_cache_append(
+            _ptr(k), _ptr(v), _ptr(q), _Strides[9](*ks, *vs, *qs), DTYPES[dtype], _ptr(freqs), R,
+            int(neighbours), _ptr(positions), _ptr(k_cache), _ptr(v_cache), layout, _ptr(pages),
+            pages.shape[1], _ptr(starts), _ptr(lengths), B, N, Hq, _ptr(out), _stream(dev)))
+    return out
+
+
+def tree_workspace_bytes(B, N, Hq, Hk, D):
+    return lib().ts_cache_attend_workspace_bytes(B, N, Hq, Hk, D)
+
+
+def tree_attention(q, k_cache, v_cache, pages, starts, parents=None, lengths=None, scale=None,
+                   out=None, ws=None):
+    """(out [B, N, Hq, D] of q's type, lse float32 [B, N, Hq]): attention of drafted tokens' queries q
+    [B, N, Hq, D] over the paged caches [P, S, Hk, D] (see cache_append), which hold starts[b] slots
+    from before and then the drafts.  Draft i sees the slots before the drafts, itself and the drafts
+    that it follows: parents (int32 [B, N]) names the one that it continues, -1 where that is the text
+    before them; without parents they are a path.  N is at most 256.  scale: of the scores, 1 /
+    sqrt(D) where it is not given.  out is 0 and lse -inf for padding (drafts from lengths[b] on)."""
+    q, qs = _prep_heads(q, "q")
+    B, N, Hq, D = q.shape
+    dtype, dev = q.dtype, q.device
+    layout, pages, starts, lengths = _prep_cache(k_cache, v_cache, pages, starts, lengths, B, dtype,
+                                                 dev)
+    if k_cache.shape[3] != D:
+        raise ValueError(f"the caches must be [P, S, Hk, {D}]")
+    parents = _prep_small(parents, "parents", torch.int32, (B, N), dev)
+    if out is None:
+        o = torch.empty((B, N, Hq, D), dtype=dtype, device=dev)
+        lse = torch.empty((B, N, Hq), dtype=torch.float32, device=dev)
+    else:
+        o, lse = _check_outs(out, ("out", "lse"), (dtype, torch.float32),
+                             ((B, N, Hq, D), (B, N, Hq)), dev)
+    if ws is not None:
+        if ws.device != dev or not ws.is_contiguous():
+            raise ValueError("ws must be a contiguous tensor on the same device as q")
+        w, nb = ws, ws.numel() * ws.element_size()
+    else:
+        nb = tree_workspace_bytes(B, N, Hq, k_cache.shape[2], D)
+        w = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
+    with _device(dev):
+        _check(lib().ts_cache_attend(
+            _ptr(q), _Strides[3](*qs), DTYPES[dtype], _ptr(k_cache), _ptr(v_cache), layout,
+            _ptr(pages), pages.shape[1], _ptr(starts), _ptr(parents), _ptr(lengths), B, N, Hq,
+            D ** -0.5 if scale is None else scale, _ptr(o), _ptr(lse), _ptr(w), nb, _stream(dev)))
+    return o, lse

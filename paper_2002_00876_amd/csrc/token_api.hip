@@ -4,45 +4,15 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <cstdlib>
-#include <cstring>
-#include <exception>
 #include <string>
 #include <vector>
 
-#include "internal.h"
+#include "call_checks.h"
 #include "token.h"
 #include "token_calls.h"
 
 namespace tsc {
 namespace {
-
-constexpr int64_t kMaxRows = (int64_t)1 << 29;
-constexpr int64_t kMaxStride = (int64_t)1 << 40;
-
-bool checked() {
-    const char* env = std::getenv("TS_CHECK");
-    return env && std::strcmp(env, "1") == 0;
-}
-
-// Runs a call's body; nothing is thrown through the C boundary
-template <class F>
-ts_status guarded(F f) {
-    try {
-        return f();
-    } catch (const std::exception&) {
-        return TS_ERR_HIP;   // host memory ran out while a check or a message was being made
-    }
-}
-
-ts_status bad(const char* call, ts_status code, const std::string& what) {
-    return report_error(code, (std::string(call) + ": " + what).c_str());
-}
-
-ts_status done(const char* call, hipError_t e) {
-    if (e == hipSuccess) return TS_OK;
-    return bad(call, TS_ERR_HIP, std::string("HIP: ") + hipGetErrorString(e));
-}
 
 bool dims_ok(int64_t B, int64_t N, int64_t V) {
     return B >= 1 && N >= 1 && V >= 1 && V <= kMaxVocab && B <= kMaxRows && N <= kMaxRows &&
@@ -63,12 +33,6 @@ ts_status check_top(const char* call, int64_t V, int64_t K) {
                                          ")] (got " + std::to_string(K) + ")");
 }
 
-ts_status check_type(const char* call, const char* name, int dtype) {
-    if (dtype >= TS_FLOAT32 && dtype <= TS_FLOAT16) return TS_OK;
-    return bad(call, TS_ERR_BAD_ARG, std::string(name) + " has no element type of code " +
-                                         std::to_string(dtype));
-}
-
 ts_status check_rows(const char* call, const char* name, int dtype, int64_t sb, int64_t sn) {
     if (ts_status st = check_type(call, name, dtype)) return st;
     if (sb >= 0 && sn >= 0 && sb <= kMaxStride && sn <= kMaxStride) return TS_OK;
@@ -80,37 +44,6 @@ ts_status check_temperature(const char* call, const char* name, float t) {
     // 1 / T and log2(e) / T have to be normal floats, and every finite logit's quotient a sum
     if (t >= 1e-6f && t <= 1e6f) return TS_OK;
     return bad(call, TS_ERR_BAD_ARG, std::string(name) + " must be in [1e-6, 1e6]");
-}
-
-ts_status check_ptr(const char* call, const char* name, const void* p) {
-    if (p) return TS_OK;
-    return bad(call, TS_ERR_NULL_ARG, std::string(name) + " is NULL");
-}
-
-ts_status check_ws(const char* call, size_t need, const void* ws, size_t ws_bytes) {
-    if (need == 0) return TS_OK;
-    if (!ws) return bad(call, TS_ERR_NULL_ARG, "ws is NULL");
-    if (ws_bytes >= need && reinterpret_cast<uintptr_t>(ws) % 256 == 0) return TS_OK;
-    return bad(call, TS_ERR_WORKSPACE, "the workspace needs " + std::to_string(need) +
-                                           " bytes aligned to 256 (got " +
-                                           std::to_string(ws_bytes) + ")");
-}
-
-// TS_CHECK=1: lengths within [0, N], read on the host; len keeps them
-ts_status check_lengths(const char* call, const int32_t* lengths, int64_t B, int64_t N,
-                        hipStream_t s, std::vector<int32_t>* len) {
-    len->assign((size_t)B, (int32_t)N);
-    if (!lengths) return TS_OK;
-    if (hipMemcpyAsync(len->data(), lengths, sizeof(int32_t) * B, hipMemcpyDeviceToHost, s) !=
-            hipSuccess ||
-        hipStreamSynchronize(s) != hipSuccess)
-        return bad(call, TS_ERR_HIP, "could not read lengths for TS_CHECK");
-    for (int64_t b = 0; b < B; ++b)
-        if ((*len)[b] < 0 || (*len)[b] > N)
-            return bad(call, TS_ERR_LENGTHS, "lengths[" + std::to_string(b) + "] = " +
-                                                 std::to_string((*len)[b]) +
-                                                 " is outside [0, N]");
-    return TS_OK;
 }
 
 // TS_CHECK=1: W whole numbers of every row within [lo, V), no two of a row alike where
