@@ -3,6 +3,8 @@
  * what a chain needs beside a large model.
  *   - the K largest logits of every row and its log-sum-exp: what a teacher leaves behind;
  *   - the divergence of a student's rows from a teacher's top logits, and its gradient;
+ *   - the log-probabilities of given tokens, rows' entropies and most likely tokens, and the
+ *     gradient of the first two;
  *   - the verification of drafted tokens (a chain's samples, for instance) against the
  *     target's probabilities, from given random numbers.
  * Status codes, errors, ownership, streams and reproducibility are those of ts_chain.h: every
@@ -46,6 +48,8 @@ extern "C" {
 #define TS_TOKEN_DISTILL 1
 #define TS_TOKEN_DISTILL_GRAD 2
 #define TS_TOKEN_VERIFY 3 /* N: the most drafts of a sequence; K is ignored */
+#define TS_TOKEN_SCORE 4 /* K may be 0 */
+#define TS_TOKEN_SCORE_GRAD 5 /* K is ignored */
 
 /* Largest V and largest K. */
 int ts_token_max_vocab(void);
@@ -114,6 +118,42 @@ ts_status ts_token_distill_grad(const void* logits, int dtype, int64_t stride_b,
                                 const float* weights, const int32_t* lengths, int64_t B,
                                 int64_t N, int64_t V, int64_t K, float temperature, float* loss,
                                 void* grad, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Scores of given tokens, with p = softmax(logits / T) of every row.
+ *   tokens   int32 [B, N].  One outside [0, V) has no score.
+ *   K        >= 0: alternatives asked for.
+ *   logp     float32 [B, N]: log p(token); 0 where there is none.
+ *   entropy  float32 [B, N]: - sum_v p_v log p_v.
+ *   alternatives      int32 [B, N, K]: the K most likely tokens, the most likely first, equal ones by the
+ *                     lowest index (the given token among them where it is one).  May be NULL when K == 0.
+ *   alternative_logp  float32 [B, N, K]: log p of these.  May be NULL when K == 0.
+ * Padding: logp and entropy 0, alternatives -1, alternative_logp -inf.  A row without a finite logit
+ * has log p = -inf throughout, and entropy 0.
+ */
+ts_status ts_token_score(const void* logits, int dtype, int64_t stride_b, int64_t stride_n,
+                         const int32_t* tokens, const int32_t* lengths, int64_t B, int64_t N,
+                         int64_t V, int64_t K, float temperature, float* logp, float* entropy,
+                         int32_t* alternatives, float* alternative_logp, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/*
+ * The first two with a gradient.
+ *   weights, entropy_weights  float32 [B, N] or NULL (all 1; all 0): the derivatives of what is
+ *            maximised by each row's log p(token) and by its entropy (-1 / rows and 0 for a mean
+ *            negative log-likelihood that is minimised).
+ *   logp, entropy  float32 [B, N] or NULL: as above, not weighted.
+ *   grad     [B, N, V], contiguous, of the logits' type, not overlapping them:
+ *            (weights ([v = token] - p_v) - entropy_weights p_v (log p_v + entropy)) / T,
+ *            rounded once; without the first term where the row's token has no score.  Exactly 0 for
+ *            padding and for rows without a finite logit.
+ */
+ts_status ts_token_score_grad(const void* logits, int dtype, int64_t stride_b, int64_t stride_n,
+                              const int32_t* tokens, const float* weights,
+                              const float* entropy_weights, const int32_t* lengths, int64_t B,
+                              int64_t N, int64_t V, float temperature, float* logp,
+                              float* entropy, void* grad, void* ws, size_t ws_bytes,
+                              void* stream);
 
 /*
  * Verification of drafted tokens (speculative sampling): what is emitted is distributed as the

@@ -14,6 +14,7 @@ LIB_PATH = os.path.join(HERE, "libtschain.so")
 OP_LOGPARTITION, OP_MARGINALS, OP_VITERBI, OP_MARGINALS_VITERBI = 0, 1, 2, 3
 OP_ENTROPY, OP_LOG_DENSITY, OP_SAMPLE = 4, 5, 6
 TOKEN_TOP, TOKEN_DISTILL, TOKEN_DISTILL_GRAD, TOKEN_VERIFY = 0, 1, 2, 3
+TOKEN_SCORE, TOKEN_SCORE_GRAD = 4, 5
 STATUS = {0: "TS_OK", -1: "TS_ERR_NULL_ARG", -2: "TS_ERR_BAD_DIM", -3: "TS_ERR_WORKSPACE",
           -4: "TS_ERR_LENGTHS", -5: "TS_ERR_HIP", -6: "TS_ERR_LABELS",
           -7: "TS_ERR_BAD_ARG"}
@@ -72,6 +73,10 @@ def lib():
                                             f32, p, p, p, sz, p]
         L.ts_token_verify.argtypes = [p, ci, i64, i64, p, ci, i64, i64, p, p, p, p, p, i64, i64,
                                       i64, f32, f32, p, p, p, p, sz, p]
+        L.ts_token_score.argtypes = [p, ci, i64, i64, p, p, i64, i64, i64, i64, f32, p, p, p, p, p, sz,
+                                     p]
+        L.ts_token_score_grad.argtypes = [p, ci, i64, i64, p, p, p, p, i64, i64, i64, f32, p, p, p, p,
+                                          sz, p]
         strides, layout = ctypes.POINTER(i64), ctypes.POINTER(CacheLayout)
         L.ts_cache_max_head.restype = ci
         L.ts_cache_max_nodes.restype = ci
@@ -81,7 +86,7 @@ def lib():
         L.ts_cache_attend_workspace_bytes.restype = sz
         L.ts_cache_attend.argtypes = [p, strides, ci, p, p, layout, p, i64, p, p, p, i64, i64, i64,
                                       f32, p, p, p, sz, p]
-        for f in ("ts_cache_append", "ts_cache_attend", "ts_token_top", "ts_token_distill", "ts_token_distill_grad", "ts_token_verify",
+        for f in ("ts_token_score", "ts_token_score_grad", "ts_cache_append", "ts_cache_attend", "ts_token_top", "ts_token_distill", "ts_token_distill_grad", "ts_token_verify",
                   "ts_chain_logpartition", "ts_chain_marginals", "ts_chain_viterbi",
                   "ts_chain_marginals_noalloc",
                   "ts_chain_marginals_viterbi", "ts_chain_entropy", "ts_chain_log_density",
@@ -463,6 +468,71 @@ def distill_grad(logits, top_values, top_indices, top_lse=None, lengths=None, we
                                        temperature, _ptr(loss) if want_loss else None, _ptr(grad),
                                        _ptr(w), nb, _stream(dev)))
     return (loss if want_loss else None), grad
+
+
+def score(logits, tokens, K=0, lengths=None, temperature=1.0, out=None, ws=None):
+    """(logp [B, N], entropy [B, N], alternatives int32 [B, N, K], alternative_logp [B, N, K]), float32
+    where nothing else is said: the log-probability of each row's given token (int32 [B, N]) under
+    softmax(logits / temperature), logits [B, N, V], the row's entropy, and its K most likely tokens
+    with theirs, the most likely first and equal ones by the lowest index.  A token outside the
+    vocabulary has no score (0).  Rows from lengths (int32 [B]) on are padding: logp and entropy 0,
+    alternatives -1 and -inf.  The scores have no graph: score_grad() is their backward pass."""
+    logits, dtype, sb, sn = _prep_rows(logits, "logits")
+    B, N, V = logits.shape
+    dev = logits.device
+    tokens = _prep_small(tokens, "tokens", torch.int32, (B, N), dev)
+    lengths = _prep_small(lengths, "lengths", torch.int32, (B,), dev)
+    if K < 0:
+        raise ValueError("K must be >= 0")
+    if out is None:
+        logp = torch.empty((B, N), dtype=torch.float32, device=dev)
+        entropy = torch.empty((B, N), dtype=torch.float32, device=dev)
+        alternatives = torch.empty((B, N, K), dtype=torch.int32, device=dev)
+        alternative_logp = torch.empty((B, N, K), dtype=torch.float32, device=dev)
+    else:
+        f32 = torch.float32
+        logp, entropy, alternatives, alternative_logp = _check_outs(
+            out, ("logp", "entropy", "alternatives", "alternative_logp"),
+            (f32, f32, torch.int32, f32), ((B, N), (B, N), (B, N, K), (B, N, K)), dev)
+    w, nb = _token_workspace(TOKEN_SCORE, B, N, V, K, dev, ws)
+    with _device(dev):
+        _check(lib().ts_token_score(_ptr(logits), dtype, sb, sn, _ptr(tokens), _ptr(lengths), B, N, V,
+                                    K, temperature, _ptr(logp), _ptr(entropy), _ptr(alternatives),
+                                    _ptr(alternative_logp), _ptr(w), nb, _stream(dev)))
+    return logp, entropy, alternatives, alternative_logp
+
+
+def score_grad(logits, tokens, lengths=None, weights=None, entropy_weights=None, temperature=1.0,
+               out=None, ws=None, want_scores=True):
+    """(logp [B, N], entropy [B, N], both None without want_scores, grad [B, N, V] of the logits' type):
+    the gradient of sum(weights * logp + entropy_weights * entropy) by the logits, weights and
+    entropy_weights float32 [B, N] (None: all 1, and all 0).  0 for padding."""
+    logits, dtype, sb, sn = _prep_rows(logits, "logits")
+    B, N, V = logits.shape
+    dev = logits.device
+    tokens = _prep_small(tokens, "tokens", torch.int32, (B, N), dev)
+    lengths = _prep_small(lengths, "lengths", torch.int32, (B,), dev)
+    weights = _prep_small(weights, "weights", torch.float32, (B, N), dev)
+    entropy_weights = _prep_small(entropy_weights, "entropy_weights", torch.float32, (B, N), dev)
+    logp = entropy = None
+    if out is None:
+        if want_scores:
+            logp = torch.empty((B, N), dtype=torch.float32, device=dev)
+            entropy = torch.empty((B, N), dtype=torch.float32, device=dev)
+        grad = torch.empty((B, N, V), dtype=logits.dtype, device=dev)
+    else:
+        logp, entropy, grad = _check_outs(
+            out, ("logp", "entropy", "grad"), (torch.float32, torch.float32, logits.dtype),
+            ((B, N), (B, N), (B, N, V)), dev)
+        if not want_scores:
+            logp = entropy = None
+    w, nb = _token_workspace(TOKEN_SCORE_GRAD, B, N, V, 1, dev, ws)
+    with _device(dev):
+        _check(lib().ts_token_score_grad(_ptr(logits), dtype, sb, sn, _ptr(tokens), _ptr(weights),
+                                         _ptr(entropy_weights), _ptr(lengths), B, N, V, temperature,
+                                         _ptr(logp), _ptr(entropy), _ptr(grad), _ptr(w), nb,
+                                         _stream(dev)))
+    return logp, entropy, grad
 
 
 def verify(target, draft, tokens, uniforms, noise, lengths=None, draft_lse=None, temperature=1.0,

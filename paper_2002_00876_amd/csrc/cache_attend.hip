@@ -26,7 +26,6 @@ constexpr int kSplitBatch = 512;      // most sequences whose slots are divided 
 constexpr int kWant = 512;            // workgroups that fill the chip
 constexpr float kLow = -1e30f;        // below every score
 constexpr float kNone = -1e36f;       // where a running maximum begins: below kLow * scale, the floats far
-constexpr float kLn2 = 0.693147180559945f;
 
 // Numerators are at most 2^kUp: float16's smallest normal number would otherwise be 2^-14 of the
 // largest, and a long context's many small ones would lose their digits or vanish.

@@ -277,6 +277,104 @@ __device__ __forceinline__ float max_of(const float (&v)[W]) {
     }
 }
 
+// The same with the entropy's sum beside it: t = sum of d 2^d over exponents d = (x - m) c, none of them
+// positive, so that the row's entropy log s - t ln 2 / s is made of two terms that are not negative.
+// Exponents below -200, whose numerators are 0, count as that: 0 times -inf would be no number.
+struct Spread {
+    float m, s, t;
+    __device__ __forceinline__ Soft soft() const { return {m, s}; }
+};
+constexpr float kNoTerm = -200.f;
+constexpr float kLn2 = 0.693147180559945f;
+__device__ __forceinline__ Spread spread_empty() { return {-FLT_MAX, 0.f, 0.f}; }
+// a's sums as those of a maximum m that is not below its own
+__device__ __forceinline__ Spread spread_raise(Spread a, float m, float c) {
+#pragma clang fp contract(off)
+    const float d = fmaxf((a.m - m) * c, kNoTerm), f = exp2_(d);
+    return {m, a.s * f, (a.t + a.s * d) * f};
+}
+template <int W>
+__device__ __forceinline__ void spread_push(Spread& a, const float (&v)[W], float c) {
+#pragma clang fp contract(off)
+    float m = a.m;
+#pragma unroll
+    for (int k = 0; k < W; ++k) m = fmaxf(m, v[k]);
+    a = spread_raise(a, m, c);
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+        const float d = fmaxf((v[k] - m) * c, kNoTerm), e = exp2_(d);
+        a.s += e;
+        a.t += d * e;
+    }
+}
+__device__ __forceinline__ Spread wave_spread(Spread a, float c) {
+    const float m = wave_max_fast(a.m);
+    a = spread_raise(a, m, c);
+    return {m, wave_sum_fast(a.s), wave_sum_fast(a.t)};
+}
+// Every thread gets the workgroup's; red holds NT / 64 of them and is free again on return
+template <int NT>
+__device__ __forceinline__ Spread block_spread(Spread a, float c, float4* red) {
+    a = wave_spread(a, c);
+    if constexpr (NT == kWave) return a;
+    const int lane = threadIdx.x % kWave;
+    if (lane == 0) red[threadIdx.x / kWave] = make_float4(a.m, a.s, a.t, 0.f);
+    __syncthreads();
+    const float4 r = lane < NT / kWave ? red[lane] : make_float4(-FLT_MAX, 0.f, 0.f, 0.f);
+    __syncthreads();
+    return wave_spread({r.x, r.y, r.z}, c);
+}
+
+// ChunkSoft's sums with the entropy's
+struct ChunkSpread {
+    float m, r, s, t;
+    __device__ __forceinline__ void init(const Scale& k) {
+#pragma clang fp contract(off)
+        m = -k.most, r = m * k.c, s = t = 0.f;
+    }
+    __device__ __forceinline__ void raise(float most, float c) {
+#pragma clang fp contract(off)
+        if (most > m) {
+            const float r2 = most * c, d = fmaxf(r - r2, kNoTerm), f = exp2_(d);
+            t = (t + s * d) * f;
+            s *= f;
+            m = most;
+            r = r2;
+        }
+    }
+    template <int W>
+    __device__ __forceinline__ void push(const float (&v)[W], float c) {
+        float e[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            const float d = fmaxf(fmaf(v[k], c, -r), kNoTerm);
+            e[k] = exp2_(d);
+            t = fmaf(d, e[k], t);
+        }
+#pragma unroll
+        for (int d = W / 2; d > 0; d /= 2)
+#pragma unroll
+            for (int k = 0; k < d; ++k) e[k] += e[k + d];
+        s += e[0];
+    }
+    __device__ __forceinline__ Spread value(float c) const {
+#pragma clang fp contract(off)
+        if (!(s > 0.f)) return spread_empty();
+        const float d = -fmaf(m, c, -r), f = exp2_(d);   // what r was rounded by
+        return {m, s * f, (t + s * d) * f};
+    }
+};
+
+// What a row's scores are made of, from the sums of its softmax: log p_v = (x_v - m) / T - ls, and the
+// entropy.  The largest logit's own numerator is 1: a sum below that is rounding.  A row without a finite
+// logit has no p: its log p are -inf, its entropy 0.
+struct RowScore {
+    float m, ls, entropy;
+    __device__ __forceinline__ explicit RowScore(Spread a)
+        : m(a.m), ls(logf(fmaxf(a.s, 1.f))), entropy(ls - kLn2 * fminf(a.t, 0.f) / fmaxf(a.s, 1.f)) {}
+    __device__ __forceinline__ float logp(float x, float inv_t) const { return (x - m) * inv_t - ls; }
+};
+
 // log sum exp(x / T) of a row; -inf where it has no finite logit
 __device__ __forceinline__ float soft_lse(Soft a, float inv_t) {
     return a.s > 0.f ? fmaf(a.m, inv_t, logf(a.s)) : -INFINITY;

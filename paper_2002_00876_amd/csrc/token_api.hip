@@ -1,6 +1,6 @@
 // token_api.hip -- the C ABI declared in include/ts_token.h: argument checks, workspace sizes
-// and the choice of kernels.  The kernels are in token_top.hip, token_distill.hip and
-// token_verify.hip.
+// and the choice of kernels.  The kernels are in token_top.hip, token_distill.hip, token_score.hip
+// and token_verify.hip.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -117,8 +117,10 @@ int ts_token_max_top(void) { return kMaxTop; }
 size_t ts_token_workspace_bytes(int op, int64_t B, int64_t N, int64_t V, int64_t K) {
     if (op == TS_TOKEN_VERIFY)
         return N >= 0 && N < kMaxRows && dims_ok(B, N + 1, V) ? verify_workspace(B, N, V) : 0;
+    if (op == TS_TOKEN_SCORE_GRAD || (op == TS_TOKEN_SCORE && K == 0))
+        return dims_ok(B, N, V) ? score_workspace(B, N, V) : 0;
     if (!dims_ok(B, N, V) || K < 1 || K > V || K > kMaxTop) return 0;
-    if (op == TS_TOKEN_TOP) return top_workspace(B, N, V, K);
+    if (op == TS_TOKEN_TOP || op == TS_TOKEN_SCORE) return top_workspace(B, N, V, K);
     if (op == TS_TOKEN_DISTILL || op == TS_TOKEN_DISTILL_GRAD)
         return distill_workspace(op, B, N, V, K);
     return 0;
@@ -144,7 +146,7 @@ ts_status ts_token_top(const void* logits, int dtype, int64_t stride_b, int64_t 
             if ((st = check_lengths(call, lengths, B, N, s, &len))) return st;
         }
         const TopArgs a{{logits, stride_b, stride_n}, dtype, lengths, B, N, (int)V, (int)K,
-                        make_scale(temperature), values, indices, lse, ws};
+                        make_scale(temperature), values, indices, lse, ws, nullptr, nullptr, nullptr};
         return done(call, launch_top(a, s));
     });
 }
@@ -191,6 +193,77 @@ ts_status ts_token_distill_grad(const void* logits, int dtype, int64_t stride_b,
         a.grad = grad;
         return distill_call("ts_token_distill_grad", a, dtype, top_dtype, K, temperature,
                             TS_TOKEN_DISTILL_GRAD, ws, ws_bytes, stream);
+    });
+}
+
+ts_status ts_token_score(const void* logits, int dtype, int64_t stride_b, int64_t stride_n,
+                         const int32_t* tokens, const int32_t* lengths, int64_t B, int64_t N,
+                         int64_t V, int64_t K, float temperature, float* logp, float* entropy,
+                         int32_t* alternatives, float* alternative_logp, void* ws,
+                         size_t ws_bytes, void* stream) {
+    return guarded([&]() -> ts_status {
+        const char* call = "ts_token_score";
+        ts_status st;
+        if ((st = check_dims(call, B, N, V)) || (K && (st = check_top(call, V, K))) ||
+            (st = check_rows(call, "logits", dtype, stride_b, stride_n)) ||
+            (st = check_temperature(call, "temperature", temperature)) ||
+            (st = check_ptr(call, "logits", logits)) || (st = check_ptr(call, "tokens", tokens)) ||
+            (st = check_ptr(call, "logp", logp)) || (st = check_ptr(call, "entropy", entropy)) ||
+            (K && ((st = check_ptr(call, "alternatives", alternatives)) ||
+                   (st = check_ptr(call, "alternative_logp", alternative_logp)))) ||
+            (st = check_ws(call, ts_token_workspace_bytes(TS_TOKEN_SCORE, B, N, V, K), ws, ws_bytes)))
+            return st;
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        if (checked()) {
+            std::vector<int32_t> len;
+            if ((st = check_lengths(call, lengths, B, N, s, &len))) return st;
+        }
+        if (K) {
+            const TopArgs a{{logits, stride_b, stride_n}, dtype, lengths, B, N, (int)V, (int)K,
+                            make_scale(temperature), alternative_logp, alternatives, nullptr, ws,
+                            tokens, logp, entropy};
+            return done(call, launch_top(a, s));
+        }
+        ScoreArgs a{};
+        a.logits = {logits, stride_b, stride_n};
+        a.tokens = tokens;
+        a.lengths = lengths;
+        a.B = B;
+        a.N = N;
+        a.logp = logp;
+        a.entropy = entropy;
+        a.V = (int)V;
+        a.dtype = dtype;
+        a.scale = make_scale(temperature);
+        a.ws = ws;
+        return done(call, launch_score(a, s));
+    });
+}
+
+ts_status ts_token_score_grad(const void* logits, int dtype, int64_t stride_b, int64_t stride_n,
+                              const int32_t* tokens, const float* weights,
+                              const float* entropy_weights, const int32_t* lengths, int64_t B,
+                              int64_t N, int64_t V, float temperature, float* logp,
+                              float* entropy, void* grad, void* ws, size_t ws_bytes,
+                              void* stream) {
+    return guarded([&]() -> ts_status {
+        const char* call = "ts_token_score_grad";
+        ts_status st;
+        if ((st = check_dims(call, B, N, V)) ||
+            (st = check_rows(call, "logits", dtype, stride_b, stride_n)) ||
+            (st = check_temperature(call, "temperature", temperature)) ||
+            (st = check_ptr(call, "logits", logits)) || (st = check_ptr(call, "tokens", tokens)) ||
+            (st = check_ptr(call, "grad", grad)) ||
+            (st = check_ws(call, score_workspace(B, N, V), ws, ws_bytes)))
+            return st;
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        if (checked()) {
+            std::vector<int32_t> len;
+            if ((st = check_lengths(call, lengths, B, N, s, &len))) return st;
+        }
+        const ScoreArgs a{{logits, stride_b, stride_n}, tokens, weights, entropy_weights, lengths, B, N,
+                          logp, entropy, grad, (int)V, dtype, make_scale(temperature), ws};
+        return done(call, launch_score(a, s));
     });
 }
 

@@ -30,10 +30,13 @@ struct TopArgs {
     int64_t B, N;
     int V, K;
     Scale scale;
-    void* values;
+    void* values;             // with tokens: their log-probabilities, float32
     int32_t* indices;
     float* lse;
     void* ws;
+    const int32_t* tokens;    // the scores of these are asked for, and the rows' entropies
+    float* logp;
+    float* entropy;
 };
 size_t top_workspace(int64_t B, int64_t N, int64_t V, int64_t K);
 hipError_t launch_top(const TopArgs& a, hipStream_t s);
@@ -54,6 +57,23 @@ struct DistillArgs {
 };
 size_t distill_workspace(int op, int64_t B, int64_t N, int64_t V, int64_t K);
 hipError_t launch_distill(const DistillArgs& a, hipStream_t s);
+
+struct ScoreArgs {
+    Rows logits;
+    const int32_t* tokens;
+    const float* weights;
+    const float* entropy_weights;
+    const int32_t* lengths;
+    int64_t B, N;
+    float* logp;
+    float* entropy;
+    void* grad;   // NULL: the scores alone
+    int V, dtype;
+    Scale scale;
+    void* ws;
+};
+size_t score_workspace(int64_t B, int64_t N, int64_t V);
+hipError_t launch_score(const ScoreArgs& a, hipStream_t s);
 
 struct VerifyArgs {
     Rows target, draft;

@@ -47,7 +47,10 @@ __device__ __forceinline__ uint64_t word_of(uint32_t key, int index) {
 template <int kWords>
 struct TopSharedOf {
     uint64_t list[kWords];
-    float2 red[16];
+    union {
+        float2 red[16];
+        float4 red4[16];
+    };
     int redi[2][16];
     int n;   // words in the list, or vectors noted
 };
@@ -92,10 +95,22 @@ __device__ uint32_t threshold(const uint32_t (&key)[J], int K, uint32_t lo, uint
     return lo;
 }
 
+// A row's log-probability of its given token, and its entropy
+template <class T>
+__device__ __forceinline__ RowScore write_score(const TopArgs& a, const T* x, uint32_t row, Spread sums) {
+    const RowScore score(sums);
+    if (threadIdx.x == 0) {
+        const int z = a.tokens[row];
+        a.logp[row] = z >= 0 && z < a.V ? score.logp(to_f(x[z]), a.scale.inv_t) : 0.f;
+        a.entropy[row] = score.entropy;
+    }
+    return score;
+}
+
 // The list's words, of logits x, each find their place among them
-template <class T, int NT, class S>
+template <class T, int NT, bool kScore, class S>
 __device__ __forceinline__ void write_places(const TopArgs& a, const T* x, uint32_t row, int n,
-                                             const S& sh) {
+                                             const S& sh, const RowScore& score) {
     T* values = (T*)a.values + (size_t)row * a.K;
     int32_t* indices = a.indices + (size_t)row * a.K;
     for (int i = threadIdx.x; i < n; i += NT) {
@@ -108,18 +123,24 @@ __device__ __forceinline__ void write_places(const TopArgs& a, const T* x, uint3
         if (place < a.K) {
             const int at = (int)~(uint32_t)w;
             const float v = of_key((uint32_t)(w >> 32));
-            values[place] = v == 0.f ? x[at] : from_f<T>(v);   // a key does not know a zero's sign
+            if constexpr (kScore)
+                ((float*)a.values)[(size_t)row * a.K + place] = score.logp(v, a.scale.inv_t);
+            else
+                values[place] = v == 0.f ? x[at] : from_f<T>(v);   // a key does not know a zero's sign
             indices[place] = at;
         }
     }
 }
 
-template <class T, int NT>
+template <class T, int NT, bool kScore>
 __device__ __forceinline__ void write_padding(const TopArgs& a, uint32_t row) {
+    using V = std::conditional_t<kScore, float, T>;
     for (int k = threadIdx.x; k < a.K; k += NT) {
-        ((T*)a.values)[(size_t)row * a.K + k] = from_f<T>(-INFINITY);
+        ((V*)a.values)[(size_t)row * a.K + k] = from_f<V>(-INFINITY);
         a.indices[(size_t)row * a.K + k] = -1;
     }
+    if constexpr (kScore)
+        if (threadIdx.x == 0) a.logp[row] = a.entropy[row] = 0.f;
     if (a.lse && threadIdx.x == 0) a.lse[row] = -INFINITY;
 }
 
@@ -145,7 +166,7 @@ __device__ __forceinline__ int append_ordered(bool hit, uint64_t word, int have,
 }
 
 // Rows of up to 64 * J logits, a wave each
-template <class T, int J>
+template <class T, int J, bool kScore>
 __global__ __launch_bounds__(kWave) void k_top_short(TopArgs a) {
     constexpr int NT = kWave;
     __shared__ TopSharedOf<kWave * J> sh;
@@ -154,7 +175,7 @@ __global__ __launch_bounds__(kWave) void k_top_short(TopArgs a) {
     for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const uint32_t b = row / N, n = row % N;
         if (n >= clamp_rows(a.lengths, b, N)) {
-            write_padding<T, NT>(a, row);
+            write_padding<T, NT, kScore>(a, row);
             continue;
         }
         const T* x = row_of<T>(a.logits, b, n);
@@ -172,10 +193,24 @@ __global__ __launch_bounds__(kWave) void k_top_short(TopArgs a) {
             key[j] = j * NT + tid < V ? key_of(v[j]) : 0u;   // 0: below every logit's
             mine = max(mine, key[j]);
         }
+        Spread sums = spread_empty();
+        if constexpr (kScore) {
+            sums.m = wave_max_fast(soft.m);
 #pragma unroll
-        for (int j = 0; j < J; ++j) soft.s += exp2_((v[j] - soft.m) * a.scale.c);
-        soft = block_soft<NT>(soft, a.scale.c, sh.red);
-        if (a.lse && tid == 0) a.lse[row] = soft_lse(soft, a.scale.inv_t);
+            for (int j = 0; j < J; ++j) {
+                const float d = fmaxf((v[j] - sums.m) * a.scale.c, kNoTerm), e = exp2_(d);
+                sums.s += e;
+                sums.t += d * e;
+            }
+            sums.s = wave_sum_fast(sums.s);
+            sums.t = wave_sum_fast(sums.t);
+        } else {
+#pragma unroll
+            for (int j = 0; j < J; ++j) soft.s += exp2_((v[j] - soft.m) * a.scale.c);
+            soft = block_soft<NT>(soft, a.scale.c, sh.red);
+            if (a.lse && tid == 0) a.lse[row] = soft_lse(soft, a.scale.inv_t);
+        }
+        const RowScore score = kScore ? write_score<T>(a, x, row, sums) : RowScore(sums);
         const int enough = 2 * K + 64;   // words that are soon counted
         uint32_t lo = 1;                 // every logit's key reaches it
         int c = V;
@@ -203,7 +238,7 @@ __global__ __launch_bounds__(kWave) void k_top_short(TopArgs a) {
                 have = append_ordered<NT>(kj == lo, word_of(lo, j * NT + tid), have, K, sh);
             }
         __syncthreads();
-        write_places<T, NT>(a, x, row, have, sh);
+        write_places<T, NT, kScore>(a, x, row, have, sh, score);
         __syncthreads();   // the list is free for the next row
     }
 }
@@ -301,7 +336,7 @@ struct TopPlan {
     int parts;
     int64_t rows;     // of a slab
     float* least;     // [rows]
-    float4* sums;     // [rows][parts]: maximum and sum of the softmax, largest logit
+    float4* sums;     // [rows][parts]: maximum and sum of the softmax, largest logit, entropy's sum
     int32_t* count;   // [rows][parts][kScanWaves]: vectors that reach the threshold
     int32_t* at;      // [rows][parts][kScanWaves][kKeep]: their numbers
     Vec4* kept;       // [rows][parts][kScanWaves][kKeep]: and what they hold
@@ -337,7 +372,10 @@ struct ScanShared {
         Vec4 kept[kScanWaves][kKeep];
     };
     int at[kScanWaves][kKeep];
-    float2 red[kScanWaves];
+    union {
+        float2 red[kScanWaves];
+        float4 red4[kScanWaves];
+    };
     float least;
 };
 
@@ -369,7 +407,7 @@ __device__ uint32_t guess(const uint32_t* keys, int K, float sampled) {
 
 // One workgroup a part of a row: sums of its softmax, and the vectors that reach the threshold.
 // They are kept in LDS until the end: the loads' waits would count their stores to memory.
-template <class T>
+template <class T, bool kScore>
 __global__ __launch_bounds__(kScanThreads, 8) void k_top_scan(TopArgs a, TopPlan p, uint32_t first,
                                                               uint32_t rows) {
     __shared__ ScanShared sh;
@@ -420,7 +458,7 @@ __global__ __launch_bounds__(kScanThreads, 8) void k_top_scan(TopArgs a, TopPlan
     const int per = ((nv + p.parts - 1) / p.parts + 7) / 8 * 8;   // whole cache lines
     const int lo = min((int)part * per, nv), hi = min(lo + per, nv);
     const float c = a.scale.c, least = sh.least;
-    ChunkSoft soft;
+    std::conditional_t<kScore, ChunkSpread, ChunkSoft> soft;
     soft.init(a.scale);
     float most = -INFINITY;
     int found = 0;   // of this wave
@@ -480,10 +518,14 @@ __global__ __launch_bounds__(kScanThreads, 8) void k_top_scan(TopArgs a, TopPlan
         soft.raise(one[0], c);
         soft.push(one, c);
     }
-    const Soft all = block_soft<NT>(soft.value(c), c, sh.red);
-    most = block_max<NT>(most, (float*)sh.red);
-    if (tid == 0) {
-        p.sums[blockIdx.x] = make_float4(all.m, all.s, most, 0.f);
+    if constexpr (kScore) {
+        const Spread all = block_spread<NT>(soft.value(c), c, sh.red4);
+        most = block_max<NT>(most, (float*)sh.red);
+        if (tid == 0) p.sums[blockIdx.x] = make_float4(all.m, all.s, most, all.t);
+    } else {
+        const Soft all = block_soft<NT>(soft.value(c), c, sh.red);
+        most = block_max<NT>(most, (float*)sh.red);
+        if (tid == 0) p.sums[blockIdx.x] = make_float4(all.m, all.s, most, 0.f);
     }
     const size_t q = (size_t)blockIdx.x * kScanWaves + wave;
     if (lane == 0) p.count[q] = found;
@@ -516,7 +558,7 @@ __device__ uint32_t group_threshold(const T* row, int V, int K, TopShared& sh) {
 }
 
 // One workgroup a row: the list from the kept vectors
-template <class T>
+template <class T, bool kScore>
 __global__ __launch_bounds__(kTopThreads) void k_top_pick(TopArgs a, TopPlan p, uint32_t first,
                                                           uint32_t rows) {
     __shared__ TopShared sh;
@@ -526,7 +568,7 @@ __global__ __launch_bounds__(kTopThreads) void k_top_pick(TopArgs a, TopPlan p, 
     if (i >= rows) return;
     const uint32_t row = first + i, b = row / (uint32_t)a.N, n = row % (uint32_t)a.N;
     if (n >= clamp_rows(a.lengths, b, a.N)) {
-        write_padding<T, NT>(a, row);
+        write_padding<T, NT, kScore>(a, row);
         return;
     }
     const T* x = row_of<T>(a.logits, b, n);
@@ -539,12 +581,16 @@ __global__ __launch_bounds__(kTopThreads) void k_top_pick(TopArgs a, TopPlan p, 
     };
     bool lost = false;
     Soft soft = soft_empty();
+    Spread sums = spread_empty();
     float most;
     {
         const int lane = tid % kWave;
         const float4 s = lane < p.parts ? p.sums[(size_t)i * p.parts + lane]
                                         : make_float4(-FLT_MAX, 0.f, -INFINITY, 0.f);
-        soft = wave_soft({s.x, s.y}, c);
+        if constexpr (kScore)
+            sums = wave_spread({s.x, s.y, s.w}, c);
+        else
+            soft = wave_soft({s.x, s.y}, c);
         most = wave_max_fast(s.z);
     }
     // the scan's waves' vectors, `each` threads to a wave's
@@ -565,7 +611,14 @@ __global__ __launch_bounds__(kTopThreads) void k_top_pick(TopArgs a, TopPlan p, 
     }
     const int e = V / W * W + tid;   // the row's last few logits
     if (e < V && to_f(x[e]) >= least) append(to_f(x[e]), e);
-    if (a.lse) {
+    if constexpr (kScore) {
+        if (far(most, a.scale)) {
+            sums = spread_empty();
+            walk_row<T, NT, 1>(x, 0, V, tid,
+                               [&](const float (&v)[W], int, int) { spread_push(sums, v, c); });
+            sums = block_spread<NT>(sums, c, sh.red4);
+        }
+    } else if (a.lse) {
         if (far(most, a.scale)) {
             soft = soft_empty();
             walk_row<T, NT, 1>(x, 0, V, tid,
@@ -574,6 +627,7 @@ __global__ __launch_bounds__(kTopThreads) void k_top_pick(TopArgs a, TopPlan p, 
         }
         if (tid == 0) a.lse[row] = soft_lse(soft, a.scale.inv_t);
     }
+    const RowScore score = kScore ? write_score<T>(a, x, row, sums) : RowScore(sums);
     lost = __syncthreads_or(lost);
     int have = sh.n;
     __syncthreads();
@@ -601,7 +655,7 @@ __global__ __launch_bounds__(kTopThreads) void k_top_pick(TopArgs a, TopPlan p, 
     // -inf is none of the K largest before every finite logit is
     if (have < K) have = append_equal<T, NT>(x, V, K, key_of(-INFINITY), have, sh);
     __syncthreads();
-    write_places<T, NT>(a, x, row, have, sh);
+    write_places<T, NT, kScore>(a, x, row, have, sh, score);
 }
 
 }  // namespace
@@ -610,30 +664,37 @@ size_t top_workspace(int64_t B, int64_t N, int64_t V, int64_t) {
     return V <= kShort ? 0 : top_plan(B * N, V, nullptr).bytes;
 }
 
-hipError_t launch_top(const TopArgs& a, hipStream_t s) {
+namespace {
+template <bool kScore>
+hipError_t launch_top_as(const TopArgs& a, hipStream_t s) {
     hipError_t e = hipSuccess;
     with_type(a.dtype, [&](auto t) {
         using T = decltype(t);
         const int64_t rows = a.B * a.N;
         const unsigned grid = row_grid(rows, kWave);
         if (a.V <= 64)
-            k_top_short<T, 1><<<grid, kWave, 0, s>>>(a);
+            k_top_short<T, 1, kScore><<<grid, kWave, 0, s>>>(a);
         else if (a.V <= 256)
-            k_top_short<T, 4><<<grid, kWave, 0, s>>>(a);
+            k_top_short<T, 4, kScore><<<grid, kWave, 0, s>>>(a);
         else if (a.V <= kShort)
-            k_top_short<T, 16><<<grid, kWave, 0, s>>>(a);
+            k_top_short<T, 16, kScore><<<grid, kWave, 0, s>>>(a);
         else {
             const TopPlan p = top_plan(rows, a.V, a.ws);
             for (int64_t first = 0; first < rows && e == hipSuccess; first += p.rows) {
                 const uint32_t n = (uint32_t)(rows - first < p.rows ? rows - first : p.rows);
                 const uint32_t at = (uint32_t)first;
-                k_top_scan<T><<<n * p.parts, kScanThreads, 0, s>>>(a, p, at, n);
-                k_top_pick<T><<<n, kTopThreads, 0, s>>>(a, p, at, n);
+                k_top_scan<T, kScore><<<n * p.parts, kScanThreads, 0, s>>>(a, p, at, n);
+                k_top_pick<T, kScore><<<n, kTopThreads, 0, s>>>(a, p, at, n);
                 e = hipGetLastError();
             }
         }
     });
     return e == hipSuccess ? hipGetLastError() : e;
+}
+}  // namespace
+
+hipError_t launch_top(const TopArgs& a, hipStream_t s) {
+    return a.tokens ? launch_top_as<true>(a, s) : launch_top_as<false>(a, s);
 }
 
 }  // namespace tsc
