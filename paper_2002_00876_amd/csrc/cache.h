@@ -15,11 +15,15 @@ __device__ __forceinline__ int slots_before(const Cache& c, int64_t b) {
     return clamp_to(c.starts[b], c.M * c.S);
 }
 
-// Elements from the caches' start to slot j's token (of head 0); -1: it is not there
-__device__ __forceinline__ int64_t slot_offset(const Cache& c, const int32_t* pages, int j) {
-    int page = (int)__umulhi((uint32_t)j, c.inv), at = j - page * c.S;
-    if (at >= c.S) ++page, at -= c.S;
-    const int id = pages[page];
+// Slot j's page, counted in its sequence's, and its place there
+__device__ __forceinline__ int page_of(const Cache& c, int j, int* at) {
+    int page = (int)__umulhi((uint32_t)j, c.inv);
+    *at = j - page * c.S;
+    if (*at >= c.S) ++page, *at -= c.S;
+    return page;
+}
+// Elements from the caches' start to token `at` of page id (of head 0); -1: it is not there
+__device__ __forceinline__ int64_t token_offset(const Cache& c, int id, int at) {
     return id >= 0 && id < c.P ? id * c.sp + at * c.st : -1;
 }
 

@@ -46,8 +46,12 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a) {
             continue;
         }
         const int slot = slots_before(a.c, b) + n;
-        const int64_t off = slot < a.c.M * a.c.S
-                                ? slot_offset(a.c, a.c.pages + (int64_t)b * a.c.M, slot) : -1;
+        int64_t off = -1;
+        if (slot < a.c.M * a.c.S) {
+            int at;
+            const int page = page_of(a.c, slot, &at);
+            off = token_offset(a.c, a.c.pages[(int64_t)b * a.c.M + page], at);
+        }
         if (tid < h) cs[tid] = cos_sin(a.positions ? a.positions[token] : slot, a.freqs[tid]);
         __syncthreads();
         // vectors of a head: its pairs (of two vectors each, or one), and what is not rotated

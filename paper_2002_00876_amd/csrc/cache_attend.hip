@@ -22,8 +22,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kWords = kMaxNodes / 32;
-constexpr int kSplitBatch = 512;      // most sequences whose slots are divided among workgroups
+constexpr int kSplitBatch = 256;      // most sequences whose slots are divided among workgroups
 constexpr int kWant = 512;            // workgroups that fill the chip
+constexpr int kWideRows = 2048;       // most rows whose parts are joined by a workgroup each
 constexpr float kLow = -1e30f;        // below every score
 constexpr float kNone = -1e36f;       // where a running maximum begins: below kLow * scale, the floats far
 
@@ -56,22 +57,40 @@ __device__ __forceinline__ S4 read_turned(const short* at) {
 
 // ---- how the slots are divided ----
 //
-// A unit is a tile's walk over KU slots.  All units of the call are cut into pieces of `per` units, so
-// that about kWant pieces make up the call whatever the lengths; a workgroup takes one piece.
+// A unit is a row tile's walk over KU slots.  The units of all row tiles, one tile after the other, make a
+// line that is cut into equal stretches, one a workgroup, whatever the lengths: none of them waits for a
+// longer one.  What a workgroup has of a row tile is written as a part where the tile goes on elsewhere; a
+// stretch has two such ends at most.
 struct AttendPlan {
-    int tiles;        // row tiles of a key head, of N drafts
-    int least;        // units of a piece, at least
-    bool split;
+    int tiles;          // row tiles of a key head, of N drafts
+    int least;          // units of a stretch, at least
+    bool split;         // otherwise a workgroup takes one row tile
     unsigned grid;
-    int* per;         // workspace: units of a piece
-    int* base;        // [B]: first part of each sequence
-    float2* ml;       // [parts][rows of a tile]: maximum (of exponents to base 2) and sum
-    float* o;         // [parts][rows of a tile][D]
+    int* per;           // workspace: units of a stretch
+    uint64_t* before;   // [B]: units of the sequences before
+    float2* ml;         // [2 * grid][rows of a tile]: maximum (of exponents to base 2) and sum
+    float* o;           // [2 * grid][rows of a tile][D]
     size_t bytes;
 };
 
+// (Values from LDS and of other lanes that are the same in all lanes, which the compiler cannot know: what
+// follows from them is scalar.)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+    return (uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)(uint32_t)x);
+}
+
+// x, of which the compiler keeps nothing ready across the loops before: their registers are needed there
+__device__ __forceinline__ int afresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// The scheduler mixes nothing from before with what comes after: their registers are not held together
+__device__ __forceinline__ void apart() { __builtin_amdgcn_sched_barrier(0); }
+
 struct Shape {
-    int rows, units, tiles, pieces;   // of a sequence: rows, units of a row tile, its row tiles, pieces
+    int rows, units, tiles;   // of a sequence: rows, units of a row tile, row tiles of a key head
 };
 
 __device__ __forceinline__ int slots_seen(const AttendArgs& a, int64_t b, int n) {
@@ -79,135 +98,133 @@ __device__ __forceinline__ int slots_seen(const AttendArgs& a, int64_t b, int n)
 }
 
 template <int TR, int KU>
-__device__ __forceinline__ Shape shape_of(const AttendArgs& a, int64_t b, int per) {
+__device__ __forceinline__ Shape shape_of(const AttendArgs& a, int64_t b) {
     const int n = new_tokens(a.c, b, a.N), G = a.Hq / a.Hk;
     Shape s;
     s.rows = n * G;
     s.tiles = (s.rows + TR - 1) / TR;
     s.units = n ? (slots_seen(a, b, n) + KU - 1) / KU : 0;
-    s.pieces = max(1, (s.units + per - 1) / per);
     return s;
 }
 
-struct Piece {
+// Units [lo, hi) of a row tile, all the same in all lanes
+struct Work {
     int64_t b;
-    int head, tile, piece, per, part;   // part < 0: the whole row
     Shape s;
+    int n, start, end;              // drafts, slots before them, all slots
+    int head, tile, lo, hi, part;   // part < 0: all of its units
+
+    __device__ __forceinline__ void of(const AttendArgs& a, int b_, Shape s_) {
+        b = b_;
+        s = {uniform(s_.rows), uniform(s_.units), uniform(s_.tiles)};
+        n = s.rows / (a.Hq / a.Hk);
+        start = uniform(slots_before(a.c, b));
+        end = min(start + n, a.c.M * a.c.S);
+    }
 };
 
-struct PlanShared {
-    uint64_t units[kWaves];
-    int sum[2][kWaves];
-    int found[3];
+struct WalkShared {
+    uint64_t before[kSplitBatch + 1];
+    uint64_t sum[kWaves];
 };
 
-// Which piece this workgroup takes; false: none
 template <int TR, int KU>
-__device__ bool find_piece(const AttendArgs& a, const AttendPlan& p, PlanShared& sh, Piece* w) {
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    int id;
-    if (!p.split) {
-        const int each = a.Hk * p.tiles;
-        const int total = (int)a.B * each, many = (total + 7) / 8;
-        id = (int)(blockIdx.x % 8) * many + (int)(blockIdx.x / 8);
-        if ((int)(blockIdx.x / 8) >= many || id >= total) return false;
-        w->b = id / each;
-        w->per = 1 << 30;
-        w->s = shape_of<TR, KU>(a, w->b, w->per);
-        id -= (int)w->b * each;
-        w->head = id / p.tiles;
-        w->tile = id % p.tiles;
-        w->piece = 0;
-        w->part = -1;
+struct Walk {
+    const AttendArgs& a;
+    const AttendPlan& p;
+    WalkShared& sh;
+    uint64_t begin, at, end;   // of the workgroup's stretch
+    int per, g;
+
+    // The stretch; every thread calls it
+    __device__ __forceinline__ Walk(const AttendArgs& a_, const AttendPlan& p_, WalkShared& sh_)
+        : a(a_), p(p_), sh(sh_) {
+        const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+        if (!p.split) {
+            const int total = (int)a.B * a.Hk * p.tiles, many = (total + 7) / 8;
+            g = (int)(blockIdx.x % 8) * many + (int)(blockIdx.x / 8);
+            begin = at = 0;
+            end = (int)(blockIdx.x / 8) < many && g < total;
+            per = 1;
+            return;
+        }
+        constexpr int kEach = kSplitBatch / kThreads;
+        uint64_t mine[kEach], all = 0;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int b = tid * kEach + k;
+            mine[k] = 0;
+            if (b < a.B) {
+                const Shape s = shape_of<TR, KU>(a, b);
+                mine[k] = (uint64_t)s.units * (s.tiles * a.Hk);
+            }
+            all += mine[k];
+        }
+        uint64_t upto = all;
+#pragma unroll
+        for (int o = 1; o < kWave; o *= 2) {
+            const uint64_t x = __shfl_up(upto, o, kWave);
+            if (lane >= o) upto += x;
+        }
+        if (lane == kWave - 1) sh.sum[wave] = upto;
+        __syncthreads();
+        uint64_t start = upto - all, total = 0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            if (i < wave) start += sh.sum[i];
+            total += sh.sum[i];
+        }
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int b = tid * kEach + k;
+            if (b < a.B) sh.before[b] = start;
+            if (blockIdx.x == 0 && b < a.B) p.before[b] = start;
+            start += mine[k];
+        }
+        total = uniform(total);
+        per = uniform(max(p.least, (int)min((total + gridDim.x - 1) / gridDim.x, (uint64_t)1 << 30)));
+        if (blockIdx.x == 0 && tid == 0) *p.per = per;
+        // workgroups of an XCD take neighbouring stretches: row tiles of the same slots share its L2
+        const int used = (int)((total + per - 1) / per), many = (used + 7) / 8;
+        g = (int)(blockIdx.x % 8) * many + (int)(blockIdx.x / 8);
+        begin = at = uniform(min((uint64_t)g * per, total));
+        end = (int)(blockIdx.x / 8) < many ? uniform(min(at + per, total)) : at;
+        __syncthreads();
+    }
+
+    __device__ __forceinline__ bool next(Work* w) {
+        if (at >= end) return false;
+        if (!p.split) {
+            const int each = a.Hk * p.tiles, b = g / each, rest = g - b * each;
+            w->of(a, b, shape_of<TR, KU>(a, b));
+            w->head = rest / p.tiles;
+            w->tile = rest % p.tiles;
+            w->lo = 0;
+            w->hi = w->s.units;
+            w->part = -1;
+            at = end;
+            return true;
+        }
+        int b = 0;
+        for (int more = (int)a.B; more - b > 1;) {   // the last sequence that begins here or before
+            const int mid = (b + more) / 2;
+            if (uniform(sh.before[mid]) <= at)
+                b = mid;
+            else
+                more = mid;
+        }
+        w->of(a, b, shape_of<TR, KU>(a, b));
+        const uint64_t in = at - uniform(sh.before[b]);
+        const int tile = uniform((int)(in >> 32 ? in / (uint32_t)w->s.units : (uint32_t)in / (uint32_t)w->s.units));
+        w->lo = (int)(in - (uint64_t)tile * w->s.units);
+        w->hi = uniform((int)min((uint64_t)w->s.units, w->lo + (end - at)));
+        w->head = tile / w->s.tiles;
+        w->tile = tile % w->s.tiles;
+        w->part = w->lo == 0 && w->hi == w->s.units ? -1 : 2 * g + (at != begin);
+        at += w->hi - w->lo;
         return true;
     }
-    constexpr int kEach = kSplitBatch / kThreads;
-    uint64_t units = 0;
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-        const int b = tid * kEach + k;
-        if (b < a.B) {
-            const Shape s = shape_of<TR, KU>(a, b, 1);
-            units += (uint64_t)s.units * s.tiles;
-        }
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) units += __shfl_xor(units, o, kWave);
-    if (lane == 0) sh.units[wave] = units;
-    __syncthreads();
-    units = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) units += sh.units[i];
-    units *= a.Hk;
-    const int per = max(p.least, (int)min((units + kWant - 1) / kWant, (uint64_t)1 << 30));
-    // workgroups and parts of the sequences before a thread's own
-    int mine[kEach], parts[kEach], all = 0, all_parts = 0;
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-        const int b = tid * kEach + k;
-        mine[k] = parts[k] = 0;
-        if (b < a.B) {
-            const Shape s = shape_of<TR, KU>(a, b, per);
-            mine[k] = a.Hk * (s.tiles * s.pieces + p.tiles - s.tiles);
-            parts[k] = s.pieces > 1 ? a.Hk * s.tiles * s.pieces : 0;
-        }
-        all += mine[k];
-        all_parts += parts[k];
-    }
-    int before = all, before_parts = all_parts;
-#pragma unroll
-    for (int o = 1; o < kWave; o *= 2) {
-        const int x = __shfl_up(before, o, kWave), y = __shfl_up(before_parts, o, kWave);
-        if (lane >= o) before += x, before_parts += y;
-    }
-    if (lane == kWave - 1) sh.sum[0][wave] = before, sh.sum[1][wave] = before_parts;
-    __syncthreads();
-    before -= all;
-    before_parts -= all_parts;
-    int total = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        if (i < wave) before += sh.sum[0][i], before_parts += sh.sum[1][i];
-        total += sh.sum[0][i];
-    }
-    // workgroups of an XCD take neighbouring pieces: row tiles of the same slots share its L2
-    const int many = (total + 7) / 8;
-    id = (int)(blockIdx.x % 8) * many + (int)(blockIdx.x / 8);
-    const bool any = (int)(blockIdx.x / 8) < many && id < total;
-#pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-        const int b = tid * kEach + k;
-        if (blockIdx.x == 0 && b < a.B) p.base[b] = before_parts;
-        if (any && id >= before && id < before + mine[k])
-            sh.found[0] = b, sh.found[1] = before, sh.found[2] = before_parts;
-        before += mine[k];
-        before_parts += parts[k];
-    }
-    if (blockIdx.x == 0 && tid == 0) *p.per = per;
-    __syncthreads();
-    if (!any) return false;
-    w->b = sh.found[0];
-    id -= sh.found[1];
-    w->per = per;
-    w->s = shape_of<TR, KU>(a, w->b, per);
-    const int working = a.Hk * w->s.tiles * w->s.pieces;
-    if (id < working) {
-        w->tile = id % w->s.tiles;
-        id /= w->s.tiles;
-        w->head = id % a.Hk;
-        w->piece = id / a.Hk;
-        w->part = w->s.pieces > 1 ? sh.found[2] + (w->head * w->s.tiles + w->tile) * w->s.pieces + w->piece
-                                  : -1;
-    } else {
-        id -= working;
-        const int rest = p.tiles - w->s.tiles;
-        w->head = id / rest;
-        w->tile = w->s.tiles + id % rest;
-        w->piece = 0;
-        w->part = -1;
-    }
-    return true;
-}
+};
 
 // ---- who sees whom ----
 
@@ -272,29 +289,79 @@ __device__ __forceinline__ uint32_t seen(const AttendArgs& a, const uint32_t* wo
     return left >= 32 ? bits : left <= 0 ? 0u : bits & ((1u << left) - 1);
 }
 
+// ---- a tile of slots in LDS ----
+//
+// Tiles go from the cache to LDS directly (a wave's load puts its lanes' 16 bytes one behind the other), so
+// rows of DP elements are not padded; instead the 16-byte chunks of a row are exchanged by its slot, so that
+// neither the sixteen rows of a score operand nor the eight of a turned read meet in a bank.
+template <int DP>
+struct Tile {
+    static constexpr int kRow = DP / 8;   // chunks of a row
+    static __device__ __forceinline__ int k_swap(int slot) { return kRow == 8 ? slot >> 1 & 7 : slot & 15; }
+    static __device__ __forceinline__ int v_swap(int slot) {
+        return kRow == 8 ? (slot >> 1 & 3) * 2 : (slot & 7) * 2;
+    }
+    // First element of a chunk.  Behind a head's end, where queries are 0 and no output is, any of the
+    // head's own will do.
+    static __device__ __forceinline__ int element(int chunk, int D) { return chunk * 8 < D ? chunk * 8 : 0; }
+};
+
+// What is read for a slot that is not there
+__device__ const Quad kZeros[kMaxHead / 8] = {};
+
+// Where a slot's keys and values of a head lie
+struct __attribute__((aligned(16))) Place {
+    const short* k;
+    const short* v;
+};
+// A slot's page is asked for while a tile is worked on, and its place made of it afterwards
+struct Page {
+    int id, at;
+    bool there;
+};
+__device__ __forceinline__ Page ask_page(const AttendArgs& a, const int32_t* pages, int j, int end) {
+    Page x;
+    x.there = j < end;
+    x.id = pages[page_of(a.c, min(j, end - 1), &x.at)];
+    return x;
+}
+__device__ __forceinline__ Place place_of(const AttendArgs& a, int head, const Page& x) {
+    const int64_t off = x.there ? token_offset(a.c, x.id, x.at) : -1, at = off + (int64_t)head * a.c.sh;
+    return off < 0 ? Place{(const short*)kZeros, (const short*)kZeros}
+                   : Place{(const short*)a.c.k + at, (const short*)a.c.v + at};
+}
+
+// 16 bytes a lane from `from` to LDS: those of the wave's lane l to `to` + 16 l, `to` the same in all.  The
+// load has no result that the compiler would wait for, which the builtin of it makes it do at the next read
+// of any LDS: loads_done() waits.  (M0 holds the LDS address and is read one state after it is written.)
+__device__ __forceinline__ void load_to_lds(const short* from, short* to) {
+    const uint32_t at = __builtin_amdgcn_readfirstlane(
+        (uint32_t)(uintptr_t)(__attribute__((address_space(3))) short*)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from)
+                 : "memory");
+}
+
+// Waits for the wave's loads to LDS (a barrier does not)
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // ---- a tile of slots against a wave's rows ----
+
+// A lane's part of the queries' operand: row r's elements 32 s + 8 (lane / 16) + (0..7)
+__device__ __forceinline__ S8 query(const AttendArgs& a, const Work& w, int r, int s) {
+    const int G = a.Hq / a.Hk, i = r / G, g = r % G, d = s * 32 + (int)threadIdx.x % kWave / 16 * 8;
+    const short* at = (const short*)a.q.p + w.b * a.q.sb + i * a.q.sn + (int64_t)(w.head * G + g) * a.q.sh;
+    return r < w.s.rows && d < a.D ? *(const S8*)(at + d) : S8{};
+}
 
 template <class T, int DP, int M, int KT>
 struct RowsOf {
-    static constexpr int KS = DP + 8, VS = DP + 16;   // row strides in LDS: no bank twice
     static constexpr int kPairs = KT / 32;
-    S8 q[M][DP / 32];
     F4 o[M][DP / 16];
     float m[M], l[M];
 
-    // first: the wave's first row of the tile's
-    __device__ __forceinline__ void load(const AttendArgs& a, const Piece& w, int first) {
-        const int lane = threadIdx.x % kWave, G = a.Hq / a.Hk;
+    __device__ __forceinline__ void init() {
 #pragma unroll
         for (int x = 0; x < M; ++x) {
-            const int r = first + x * 16 + lane % 16, i = r / G, g = r % G;
-            const short* at = (const short*)a.q.p + w.b * a.q.sb + i * a.q.sn +
-                              (int64_t)(w.head * G + g) * a.q.sh;
-#pragma unroll
-            for (int s = 0; s < DP / 32; ++s) {
-                const int d = s * 32 + lane / 16 * 8;
-                q[x][s] = r < w.s.rows && d < a.D ? *(const S8*)(at + d) : S8{};
-            }
 #pragma unroll
             for (int t = 0; t < DP / 16; ++t) o[x][t] = F4{0.f, 0.f, 0.f, 0.f};
             m[x] = kNone;
@@ -302,36 +369,42 @@ struct RowsOf {
         }
     }
 
-    // bits[x][k]: the slots k * 32 + (0..31) that the lane's row x sees
-    template <bool kMasked>
-    __device__ __forceinline__ void step(const short* K, const short* V, float c2,
-                                         const uint32_t (&bits)[M][kPairs]) {
+    // The scores of a tile in LDS
+    __device__ __forceinline__ void scores(const short* K, const S8 (&q)[M][DP / 32], F4 (&s)[M][KT / 16]) {
         const int lane = threadIdx.x % kWave, row = lane % 16, quarter = lane / 16;
-        F4 s[M][KT / 16];
+        const int swap = Tile<DP>::k_swap(row);   // (the same for row + 16)
 #pragma unroll
         for (int t = 0; t < KT / 16; ++t) {
 #pragma unroll
             for (int x = 0; x < M; ++x) s[x][t] = F4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < DP / 32; ++k) {
-                const S8 f = *(const S8*)(K + (t * 16 + row) * KS + k * 32 + quarter * 8);
+                const S8 f = *(const S8*)(K + (t * 16 + row) * DP + ((k * 4 + quarter) ^ swap) * 8);
 #pragma unroll
                 for (int x = 0; x < M; ++x) s[x][t] = mma<T>(f, q[x][k], s[x][t]);
             }
         }
-        S8 p[M][kPairs];
+    }
+
+    // Takes the scores of slots that the lane's row x does not see out; bits: slots k * 32 + (0..31)
+    static __device__ __forceinline__ void mask(F4 (&s)[KT / 16], int k, uint32_t bits) {
+        const int quarter = threadIdx.x % kWave / 16;
+#pragma unroll
+        for (int t = 2 * k; t < 2 * k + 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                s[t][e] = bits >> (t % 2 * 16 + quarter * 4 + e) & 1 ? s[t][e] : -INFINITY;
+    }
+
+    // Scores to numerators
+    __device__ __forceinline__ void numerators(F4 (&s)[M][KT / 16], S8 (&p)[M][kPairs], float c2) {
 #pragma unroll
         for (int x = 0; x < M; ++x) {
             float most = kLow;
 #pragma unroll
             for (int t = 0; t < KT / 16; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (kMasked)
-                        s[x][t][e] = bits[x][t / 2] >> (t % 2 * 16 + quarter * 4 + e) & 1
-                                         ? s[x][t][e] : -INFINITY;
-                    most = fmaxf(most, s[x][t][e]);
-                }
+                for (int e = 0; e < 4; ++e) most = fmaxf(most, s[x][t][e]);
             most = fmaxf(most, __shfl_xor(most, 16, kWave));
             most = fmaxf(most, __shfl_xor(most, 32, kWave)) * c2 - kUp<T>;
             if (__any(most > m[x])) {
@@ -353,12 +426,17 @@ struct RowsOf {
             }
             l[x] += sum;
         }
+    }
+
+    __device__ __forceinline__ void values(const short* V, const S8 (&p)[M][kPairs]) {
+        const int lane = threadIdx.x % kWave, row = lane % 16, quarter = lane / 16;
+        const int slot = quarter * 4 + row / 4, swap = Tile<DP>::v_swap(slot);   // (the same for slot + 16)
 #pragma unroll
         for (int t = 0; t < DP / 16; ++t)
 #pragma unroll
             for (int k = 0; k < kPairs; ++k) {
-                const short* at = V + (k * 32 + quarter * 4 + row / 4) * VS + t * 16 + row % 4 * 4;
-                const S4 lo = read_turned(at), hi = read_turned(at + 16 * VS);
+                const short* at = V + (k * 32 + slot) * DP + ((t * 2 + row % 4 / 2) ^ swap) * 8 + row % 2 * 4;
+                const S4 lo = read_turned(at), hi = read_turned(at + 16 * DP);
                 const S8 f = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
                 for (int x = 0; x < M; ++x) o[x][t] = mma<T>(f, p[x][k], o[x][t]);
@@ -387,31 +465,44 @@ __device__ __forceinline__ void store4(T* at, F4 v) {
     *(uint2*)at = make_uint2(w[0], w[1]);
 }
 
-// A tile's rows: element d of row r to `out`, or to a part
+// Where row r of a tile goes: to `out`, or to a part
 template <class T, int TR>
-__device__ __forceinline__ void store_row(const AttendArgs& a, const AttendPlan& p, const Piece& w, int r,
-                                          int d, F4 o, float m, float l) {
-    const int G = a.Hq / a.Hk, at = w.tile * TR + r;
-    if (w.part >= 0) {
-        if (at >= w.s.rows) return;
-        const int64_t row = (int64_t)w.part * TR + r;
-        *(F4*)(p.o + row * a.D + d) = o;
-        if (d == 0) p.ml[row] = make_float2(m, l);
-        return;
+struct Target {
+    float* part;   // its elements, or NULL
+    T* out;        // likewise
+    float f;       // what they are multiplied by
+
+    __device__ __forceinline__ Target(const AttendArgs& a, const AttendPlan& p, const Work& w, int r, float m,
+                                      float l, bool first) : part(nullptr), out(nullptr), f(1.f) {
+        const int G = a.Hq / a.Hk, at = w.tile * TR + r;
+        if (w.part >= 0) {
+            if (at >= w.s.rows) return;
+            const int64_t row = (int64_t)w.part * TR + r;
+            part = p.o + row * a.D;
+            if (first) p.ml[row] = make_float2(m, l);
+        } else if (at < a.N * G) {
+            const int64_t row = (w.b * a.N + at / G) * a.Hq + w.head * G + at % G;
+            if (at >= w.s.rows) l = 0.f;   // padding
+            f = l > 0.f ? 1.f / l : 0.f;
+            out = (T*)a.out + row * a.D;
+            if (first && a.lse) a.lse[row] = lse_of(m, l);
+        }
     }
-    if (at >= a.N * G) return;
-    const int64_t row = (w.b * a.N + at / G) * a.Hq + w.head * G + at % G;
-    const float f = l > 0.f ? 1.f / l : 0.f;
-    store4<T>((T*)a.out + row * a.D + d, o * f);
-    if (d == 0 && a.lse) a.lse[row] = lse_of(m, l);
-}
+    __device__ __forceinline__ void store(int d, F4 o) const {
+        if (part)
+            *(F4*)(part + d) = o;
+        else if (out)
+            store4<T>(out + d, o * f);
+    }
+};
 
 // Rows of a tile that are all padding
 template <class T, int TR>
-__device__ void store_padding(const AttendArgs& a, const Piece& w) {
+__device__ void store_padding(const AttendArgs& a, const Work& w) {
     const int each = a.D / 4;
     for (int i = threadIdx.x; i < TR * each; i += kThreads)
-        store_row<T, TR>(a, AttendPlan{}, w, i / each, i % each * 4, F4{0.f, 0.f, 0.f, 0.f}, 0.f, 0.f);
+        Target<T, TR>(a, AttendPlan{}, w, i / each, 0.f, 0.f, i % each == 0)
+            .store(i % each * 4, F4{0.f, 0.f, 0.f, 0.f});
 }
 
 // ---- many rows: a wave takes M * 16 of them, all share the tile of slots ----
@@ -423,95 +514,91 @@ template <class T, int DP, int M>
 struct ManyShared {
     static constexpr int KT = kTile<DP>;
     using R = RowsOf<T, DP, M, KT>;
-    short k[2][KT * R::KS];
-    short v[2][KT * R::VS];
-    int64_t off[3][KT];
-    PlanShared plan;
+    short k[2][KT * DP];
+    short v[2][KT * DP];
+    Place place[3][KT];
+    WalkShared walk;
     short up[kMaxNodes];
     uint32_t words[];   // [N][ceil(N / 32)], where there are parents
 };
 
 template <class T, int DP, int M>
-__global__ __launch_bounds__(kThreads) void k_attend_many(AttendArgs a, AttendPlan p) {
+__global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a, AttendPlan p) {
     using Shared = ManyShared<T, DP, M>;
     using R = typename Shared::R;
     constexpr int KT = Shared::KT, TR = 16 * M * kWaves, kRow = DP / 8, kPass = KT * kRow / kThreads;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Shared& sh = *(Shared*)lds;
-    Piece w;
-    if (!find_piece<TR, KT>(a, p, sh.plan, &w)) return;
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave);
+    Walk<TR, KT> walk(a, p, sh.walk);
+    Work w;
+    while (walk.next(&w)) {
     if (w.tile >= w.s.tiles) {
         store_padding<T, TR>(a, w);
-        return;
+        return;   // there is nothing behind it
     }
-    const int n = w.s.rows / (a.Hq / a.Hk), start = slots_before(a.c, w.b), end = slots_seen(a, w.b, n);
-    const int lo = w.piece * w.per, hi = min(lo + w.per, w.s.units);
+    const int n = w.n, start = w.start, end = w.end, lo = w.lo, hi = w.hi;
     if (a.parents && (int64_t)hi * KT > start) find_ancestors(a, w.b, n, sh.words, sh.up);
     const int32_t* pages = a.c.pages + w.b * a.c.M;
     const int first = w.tile * TR + wave * 16 * M;
     R rows;
-    rows.load(a, w, first);
-    auto offset = [&](int u) -> int64_t {
-        const int j = u * KT + tid;
-        return u < hi && j < end ? slot_offset(a.c, pages, j) : -1;
-    };
-    Quad k[kPass], v[kPass];
+    rows.init();
+    S8 q[M][DP / 32];
+#pragma unroll
+    for (int x = 0; x < M; ++x)
+#pragma unroll
+        for (int y = 0; y < DP / 32; ++y) q[x][y] = query(a, w, first + x * 16 + lane % 16, y);
+    auto ask = [&](int u) { return ask_page(a, pages, u * KT + tid % KT, end); };
     auto fetch = [&](int u) {
 #pragma unroll
         for (int i = 0; i < kPass; ++i) {
-            const int x = i * kThreads + tid, slot = x / kRow, d = x % kRow * 8;
-            const int64_t off = sh.off[u % 3][slot] + (int64_t)w.head * a.c.sh + d;
-            const bool there = sh.off[u % 3][slot] >= 0 && d < a.D;
-            k[i] = there ? *(const Quad*)((const short*)a.c.k + off) : Quad{};
-            v[i] = there ? *(const Quad*)((const short*)a.c.v + off) : Quad{};
+            const int x = i * kThreads + tid, slot = x / kRow, at = x % kRow;
+            const Place from = sh.place[u % 3][slot];
+            const int to = (i * kThreads + wave * kWave) * 8;
+            load_to_lds(from.k + Tile<DP>::element(at ^ Tile<DP>::k_swap(slot), a.D), sh.k[u % 2] + to);
+            load_to_lds(from.v + Tile<DP>::element(at ^ Tile<DP>::v_swap(slot), a.D), sh.v[u % 2] + to);
         }
     };
     if (tid < KT) {
-        sh.off[lo % 3][tid] = offset(lo);
-        sh.off[(lo + 1) % 3][tid] = offset(lo + 1);
+        sh.place[lo % 3][tid] = place_of(a, w.head, ask(lo));
+        sh.place[(lo + 1) % 3][tid] = place_of(a, w.head, ask(lo + 1));
     }
     __syncthreads();
     fetch(lo);
     for (int u = lo; u < hi; ++u) {
-        short *ks = sh.k[u % 2], *vs = sh.v[u % 2];
-#pragma unroll
-        for (int i = 0; i < kPass; ++i) {
-            const int x = i * kThreads + tid, slot = x / kRow, d = x % kRow * 8;
-            *(Quad*)(ks + slot * R::KS + d) = k[i];
-            *(Quad*)(vs + slot * R::VS + d) = v[i];
-        }
+        const short *ks = sh.k[u % 2], *vs = sh.v[u % 2];
+        loads_done();
         __syncthreads();
         if (u + 1 < hi) fetch(u + 1);
-        int64_t next = -1;
-        if (tid < KT) next = offset(u + 2);
-        uint32_t bits[M][R::kPairs];
-        if ((int64_t)(u + 1) * KT > start) {
+        const Page next = ask(u + 2);
+        F4 s[M][KT / 16];
+        S8 n[M][R::kPairs];
+        rows.scores(ks, q, s);
+        if ((u + 1) * KT > start) {
 #pragma unroll
-            for (int x = 0; x < M; ++x)
+            for (int x = 0; x < M; ++x) {
+                const int i = min(first + x * 16 + lane % 16, w.s.rows - 1) / (a.Hq / a.Hk);
 #pragma unroll
-                for (int y = 0; y < R::kPairs; ++y) {
-                    const int r = min(first + x * 16 + lane % 16, w.s.rows - 1);
-                    bits[x][y] = seen(a, sh.words, r / (a.Hq / a.Hk), u * KT + y * 32, start, end);
-                }
-            rows.template step<true>(ks, vs, a.c2, bits);
-        } else {
-            rows.template step<false>(ks, vs, a.c2, bits);
+                for (int y = 0; y < R::kPairs; ++y)
+                    R::mask(s[x], y, seen(a, sh.words, i, u * KT + y * 32, start, end));
+            }
         }
-        if (tid < KT) sh.off[(u + 2) % 3][tid] = next;
+        rows.numerators(s, n, a.c2);
+        rows.values(vs, n);
+        if (tid < KT) sh.place[(u + 2) % 3][tid] = place_of(a, w.head, next);
     }
     rows.finish();
+    const int own = afresh(lane);
 #pragma unroll
     for (int x = 0; x < M; ++x) {
-        const int r = wave * 16 * M + x * 16 + lane % 16;
-        const bool on = w.tile * TR + r < w.s.rows;
+        const Target<T, TR> to(a, p, w, wave * 16 * M + x * 16 + own % 16, rows.m[x], rows.l[x], own < 16);
 #pragma unroll
         for (int t = 0; t < DP / 16; ++t) {
-            const int d = t * 16 + lane / 16 * 4;
-            if (d < a.D)
-                store_row<T, TR>(a, p, w, r, d, on ? rows.o[x][t] : F4{0.f, 0.f, 0.f, 0.f}, rows.m[x],
-                                 on ? rows.l[x] : 0.f);
+            const int d = t * 16 + own / 16 * 4;
+            if (d < a.D) to.store(d, rows.o[x][t]);
         }
+    }
+    __syncthreads();   // the tiles are free for the next stretch of a row tile
     }
 }
 
@@ -521,102 +608,121 @@ template <class T, int DP, int M>
 struct FewShared {
     static constexpr int KT = 32;
     using R = RowsOf<T, DP, M, KT>;
-    struct Wave {
-        short k[KT * R::KS];
-        short v[KT * R::VS];
-    };
     union {
-        Wave wave[kWaves];
+        short v[kWaves][2][KT * DP];
         float o[kWaves][M * 16][DP];
     };
+    Place place[kWaves][2][KT];
     float2 ml[kWaves][M * 16];
-    PlanShared plan;
-    short up[kMaxNodes];
+    S8 q[M * (DP / 32)][kWave];   // the queries' operand, in the order of the lanes that use it
+    WalkShared walk;
+    short up[M * 16];
     uint32_t words[];
 };
 
 template <class T, int DP, int M>
-__global__ __launch_bounds__(kThreads) void k_attend_few(AttendArgs a, AttendPlan p) {
+__global__ __launch_bounds__(kThreads, 2) void k_attend_few(AttendArgs a, AttendPlan p) {
     using Shared = FewShared<T, DP, M>;
     using R = typename Shared::R;
     constexpr int KT = Shared::KT, KU = KT * kWaves, TR = 16 * M, kRow = DP / 8, kPass = KT * kRow / kWave;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Shared& sh = *(Shared*)lds;
-    Piece w;
-    if (!find_piece<TR, KU>(a, p, sh.plan, &w)) return;
-    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave);
+    Walk<TR, KU> walk(a, p, sh.walk);
+    Work w;
+    while (walk.next(&w)) {
     if (w.tile >= w.s.tiles) {
         store_padding<T, TR>(a, w);
-        return;
+        return;   // there is nothing behind it
     }
-    const int n = w.s.rows / (a.Hq / a.Hk), start = slots_before(a.c, w.b), end = slots_seen(a, w.b, n);
-    const int lo = w.piece * w.per, hi = min(lo + w.per, w.s.units);
+    const int n = w.n, start = w.start, end = w.end, lo = w.lo, hi = w.hi;
     if (a.parents && (int64_t)hi * KU > start) find_ancestors(a, w.b, n, sh.words, sh.up);
     const int32_t* pages = a.c.pages + w.b * a.c.M;
     R rows;
-    rows.load(a, w, w.tile * TR);
-    short *ks = sh.wave[wave].k, *vs = sh.wave[wave].v;
-    // a lane's slot of the wave's tile of unit u (its lanes' first half has one each)
-    auto offset = [&](int u) -> int64_t {
-        const int j = u * KU + wave * KT + lane % KT;
-        return u < hi && j < end ? slot_offset(a.c, pages, j) : -1;
+    rows.init();
+    for (int x = wave; x < M * (DP / 32); x += kWaves)
+        sh.q[x][lane] = query(a, w, w.tile * TR + x / (DP / 32) * 16 + lane % 16, x % (DP / 32));
+    // the places of the wave's own slots of unit u
+    auto ask = [&](int u) { return ask_page(a, pages, u * KU + wave * KT + lane % KT, end); };
+    auto keep = [&](int u, const Page& x) {
+        if (lane < KT) sh.place[wave][u % 2][lane] = place_of(a, w.head, x);
     };
-    Quad k[kPass], v[kPass];
-    auto fetch = [&](int64_t own) {
+    // Keys go to registers, as a wave's own operand, values to LDS, where they are turned
+    S8 k[KT / 16][DP / 32];
+    auto fetch_keys = [&](int u) {
 #pragma unroll
-        for (int i = 0; i < kPass; ++i) {
-            const int x = i * kWave + lane, slot = x / kRow, d = x % kRow * 8;
-            const int64_t at = __shfl(own, slot, kWave), off = at + (int64_t)w.head * a.c.sh + d;
-            const bool there = at >= 0 && d < a.D;
-            k[i] = there ? *(const Quad*)((const short*)a.c.k + off) : Quad{};
-            v[i] = there ? *(const Quad*)((const short*)a.c.v + off) : Quad{};
+        for (int t = 0; t < KT / 16; ++t) {
+            const short* from = sh.place[wave][u % 2][t * 16 + lane % 16].k;
+#pragma unroll
+            for (int y = 0; y < DP / 32; ++y)
+                k[t][y] = *(const S8*)(from + Tile<DP>::element(y * 4 + lane / 16, a.D));
         }
     };
-    fetch(offset(lo));
-    int64_t next = offset(lo + 1);
+    auto fetch_values = [&](int u) {
+#pragma unroll
+        for (int i = 0; i < kPass; ++i) {
+            const int x = i * kWave + lane, slot = x / kRow;
+            const short* from = sh.place[wave][u % 2][slot].v;
+            load_to_lds(from + Tile<DP>::element(x % kRow ^ Tile<DP>::v_swap(slot), a.D),
+                        sh.v[wave][u % 2] + i * kWave * 8);
+        }
+    };
+    keep(lo, ask(lo));
+    fetch_values(lo);
+    fetch_keys(lo);
+    keep(lo + 1, ask(lo + 1));
+    __syncthreads();   // the queries are there
     for (int u = lo; u < hi; ++u) {
-#pragma unroll
-        for (int i = 0; i < kPass; ++i) {
-            const int x = i * kWave + lane, slot = x / kRow, d = x % kRow * 8;
-            *(Quad*)(ks + slot * R::KS + d) = k[i];
-            *(Quad*)(vs + slot * R::VS + d) = v[i];
-        }
-        // the wave's own tile: its stores come before its reads without a barrier
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (u + 1 < hi) {
-            fetch(next);
-            next = offset(u + 2);
-        }
+        loads_done();
+        if (u + 1 < hi) fetch_values(u + 1);
+        apart();
         const int at = u * KU + wave * KT;
-        uint32_t bits[M][1];
+        F4 s[M][KT / 16];
+#pragma unroll
+        for (int x = 0; x < M; ++x)
+#pragma unroll
+            for (int t = 0; t < KT / 16; ++t) s[x][t] = F4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int y = 0; y < DP / 32; ++y)
+#pragma unroll
+            for (int x = 0; x < M; ++x) {
+                const S8 q = sh.q[x * (DP / 32) + y][lane];
+#pragma unroll
+                for (int t = 0; t < KT / 16; ++t) s[x][t] = mma<T>(k[t][y], q, s[x][t]);
+            }
+        apart();
+        if (u + 1 < hi) fetch_keys(u + 1);
+        const Page next = ask(u + 2);
+        apart();
         if (at < end) {
+            S8 n[M][1];
             if (at + KT > start) {
 #pragma unroll
                 for (int x = 0; x < M; ++x) {
                     const int r = min(w.tile * TR + x * 16 + lane % 16, w.s.rows - 1);
-                    bits[x][0] = seen(a, sh.words, r / (a.Hq / a.Hk), at, start, end);
+                    R::mask(s[x], 0, seen(a, sh.words, r / (a.Hq / a.Hk), at, start, end));
                 }
-                rows.template step<true>(ks, vs, a.c2, bits);
-            } else {
-                rows.template step<false>(ks, vs, a.c2, bits);
             }
+            rows.numerators(s, n, a.c2);
+            apart();
+            rows.values(sh.v[wave][u % 2], n);
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        keep(u + 2, next);
     }
     rows.finish();
     __syncthreads();   // the tiles make room for the waves' sums
+    const int own = afresh(lane);
 #pragma unroll
     for (int x = 0; x < M; ++x) {
-        const int r = x * 16 + lane % 16;
+        const int r = x * 16 + own % 16;
 #pragma unroll
-        for (int t = 0; t < DP / 16; ++t) *(F4*)&sh.o[wave][r][t * 16 + lane / 16 * 4] = rows.o[x][t];
-        if (lane < 16) sh.ml[wave][r] = make_float2(rows.m[x], rows.l[x]);
+        for (int t = 0; t < DP / 16; ++t) *(F4*)&sh.o[wave][r][t * 16 + own / 16 * 4] = rows.o[x][t];
+        if (own < 16) sh.ml[wave][r] = make_float2(rows.m[x], rows.l[x]);
     }
     __syncthreads();
     const int each = a.D / 4;
-    for (int i = tid; i < TR * each; i += kThreads) {
+    for (int i = afresh(tid); i < TR * each; i += kThreads) {
         const int r = i / each, d = i % each * 4;
-        const bool on = w.tile * TR + r < w.s.rows;
         float m = kNone, l = 0.f;
         F4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -627,40 +733,95 @@ __global__ __launch_bounds__(kThreads) void k_attend_few(AttendArgs a, AttendPla
             l += f * sh.ml[y][r].y;
             o += f * *(const F4*)&sh.o[y][r][d];
         }
-        store_row<T, TR>(a, p, w, r, d, on ? o : F4{0.f, 0.f, 0.f, 0.f}, m, on ? l : 0.f);
+        Target<T, TR>(a, p, w, r, m, l, d == 0).store(d, o);
+    }
+    __syncthreads();   // the sums' places are free for the next stretch of a row tile
     }
 }
 
 // ---- the parts of a row together ----
 
-// A wave a row
-template <class T, int TR, int KU>
+__device__ __forceinline__ uint32_t over(uint64_t x, int per) {   // (64-bit divisions take their time)
+    return x >> 32 ? (uint32_t)(x / (uint32_t)per) : (uint32_t)x / (uint32_t)per;
+}
+
+// A team a row: its lanes' groups take every so many of the row's parts, each lane four elements of it.  A
+// team is a wave, or where rows are few and so in many parts a workgroup.
+template <class T, int TR, int KU, bool kWide>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, AttendPlan p) {
-    const int lane = threadIdx.x % kWave, G = a.Hq / a.Hk;
-    const int64_t rows = a.B * a.N * a.Hq, step = (int64_t)gridDim.x * kWaves;
-    for (int64_t row = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave; row < rows; row += step) {
+    constexpr int kTeam = kWide ? kThreads : kWave;
+    __shared__ float tops[kWaves];
+    __shared__ F4 sums[kWaves][kWave];
+    __shared__ float weights[kWaves][kWave];
+    const int lane = threadIdx.x % kTeam, wave = threadIdx.x / kWave, G = a.Hq / a.Hk;
+    const int across = a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64;   // lanes of a group
+    const int groups = kTeam / across, mine = lane / across, d = lane % across * 4;
+    const int64_t rows = a.B * a.N * a.Hq, step = (int64_t)gridDim.x * (kThreads / kTeam);
+    const int per = *p.per;
+    for (int64_t row = (int64_t)blockIdx.x * (kThreads / kTeam) + (kWide ? 0 : wave); row < rows; row += step) {
         const int64_t b = row / ((int64_t)a.N * a.Hq);
         const int rest = (int)(row - b * a.N * a.Hq), i = rest / a.Hq, h = rest % a.Hq;
-        const Shape s = shape_of<TR, KU>(a, b, *p.per);
+        const Shape s = shape_of<TR, KU>(a, b);
         const int at = i * G + h % G, tile = at / TR;
-        if (s.pieces < 2 || tile >= s.tiles) continue;   // written as a whole
-        float m = kNone, l = 0.f;
+        int pieces = 0, first = 0, begun = 0;
+        if (tile < s.tiles) {   // (others are padding)
+            const uint64_t from = p.before[b] + (uint64_t)((h / G) * s.tiles + tile) * s.units;
+            const uint32_t g = over(from, per);
+            pieces = (int)(over(from + s.units - 1, per) - g) + 1;
+            if (pieces == 1) continue;   // written as a whole
+            if (at >= s.rows) pieces = 0;
+            // the row tile's part of the first stretch is that stretch's second, unless both begin together
+            first = 2 * (int)g;
+            begun = (uint64_t)g * per != from;
+        }
+        const int lane_d = d < a.D ? d : 0;
+        auto row_of_part = [&](int y) { return (int64_t)(first + 2 * y + (y == 0 ? begun : 0)) * TR + at % TR; };
+        float m = kNone;
+        for (int y = lane; y < pieces; y += kTeam) m = fmaxf(m, p.ml[row_of_part(y)].x);
+        m = wave_max_fast(m);
+        if constexpr (kWide) {
+            if (threadIdx.x % kWave == 0) tops[wave] = m;
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) m = fmaxf(m, tops[k]);
+        }
+        float l = 0.f;
         F4 o = {0.f, 0.f, 0.f, 0.f};
-        if (at < s.rows) {
-            const int64_t first = ((int64_t)p.base[b] + ((h / G) * s.tiles + tile) * s.pieces) * TR + at % TR;
-            for (int y = lane; y < s.pieces; y += kWave) m = fmaxf(m, p.ml[first + (int64_t)y * TR].x);
-            m = wave_max_fast(m);
-            for (int y = 0; y < s.pieces; ++y) {
-                const int64_t part = first + (int64_t)y * TR;
-                const float2 ml = p.ml[part];
-                const float f = exp2_(ml.x - m);
-                l += f * ml.y;
-                if (lane * 4 < a.D) o += f * *(const F4*)(p.o + part * a.D + lane * 4);
+        constexpr int kU = 4;   // parts asked for at once
+        for (int y = mine; y < pieces; y += kU * groups) {
+            float2 part[kU];
+            F4 x[kU];
+#pragma unroll
+            for (int k = 0; k < kU; ++k) {
+                const int64_t z = row_of_part(min(y + k * groups, pieces - 1));
+                part[k] = p.ml[z];
+                x[k] = *(const F4*)(p.o + z * a.D + lane_d);
+            }
+#pragma unroll
+            for (int k = 0; k < kU; ++k) {
+                const float f = y + k * groups < pieces ? exp2_(part[k].x - m) : 0.f;
+                l += f * part[k].y;
+                o += f * x[k];
             }
         }
-        const float f = l > 0.f ? 1.f / l : 0.f;
-        if (lane * 4 < a.D) store4<T>((T*)a.out + row * a.D + lane * 4, o * f);
+        for (int k = across; k < kWave; k *= 2) {
+            l += __shfl_xor(l, k, kWave);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k, kWave);
+        }
+        if constexpr (kWide) {
+            sums[wave][threadIdx.x % kWave] = o;
+            weights[wave][threadIdx.x % kWave] = l;
+            __syncthreads();
+            if (wave == 0) {
+                o = F4{0.f, 0.f, 0.f, 0.f}, l = 0.f;
+#pragma unroll
+                for (int k = 0; k < kWaves; ++k) o += sums[k][lane], l += weights[k][lane];
+            }
+        }
+        if (lane < across && d < a.D) store4<T>((T*)a.out + row * a.D + d, o * (l > 0.f ? 1.f / l : 0.f));
         if (lane == 0 && a.lse) a.lse[row] = lse_of(m, l);
+        if constexpr (kWide) __syncthreads();   // the sums' places are free for the next row
     }
 }
 
@@ -671,8 +832,9 @@ struct Choice {
     int few, m;
     int rows() const { return 16 * m * (few ? 1 : kWaves); }
 };
-Choice choose(int64_t N, int64_t Hq, int64_t Hk) {
+Choice choose(int64_t N, int64_t Hq, int64_t Hk, int64_t D) {
     const int64_t rows = N * (Hq / Hk);
+    if (D > 128) return {rows <= 16, 1};   // wider heads leave no registers for a second row a lane
     if (rows <= 16) return {1, 1};
     if (rows <= 32) return {1, 2};
     if (rows <= 64) return {0, 1};
@@ -680,14 +842,14 @@ Choice choose(int64_t N, int64_t Hq, int64_t Hk) {
 }
 
 AttendPlan attend_plan(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D, void* ws) {
-    const Choice c = choose(N, Hq, Hk);
+    const Choice c = choose(N, Hq, Hk, D);
     const int64_t TR = c.rows();
     AttendPlan p{};
     p.tiles = (int)((N * (Hq / Hk) + TR - 1) / TR);
     p.split = B <= kSplitBatch;
     p.least = c.few ? 1 : 2;
     const int64_t items = B * Hk * p.tiles;
-    p.grid = (unsigned)((items + (p.split ? kWant : 0) + 7) / 8 * 8);
+    p.grid = (unsigned)(p.split ? kWant : (items + 7) / 8 * 8);
     size_t off = 0;
     auto take = [&](size_t bytes) {
         char* at = (char*)ws + off;
@@ -695,10 +857,9 @@ AttendPlan attend_plan(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D, 
         return at;
     };
     if (p.split) {
-        // a row tile of several pieces has at most twice the full ones, of which there are kWant at most
-        const size_t parts = 2 * kWant;
+        const size_t parts = 2 * p.grid;
         p.per = (int*)take(sizeof(int));
-        p.base = (int*)take(sizeof(int) * B);
+        p.before = (uint64_t*)take(sizeof(uint64_t) * B);
         p.ml = (float2*)take(sizeof(float2) * parts * TR);
         p.o = (float*)take(sizeof(float) * parts * TR * D);
     }
@@ -729,22 +890,25 @@ hipError_t attend_as(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
         e = launch_lds(allow, most, k_attend_many<T, DP, M>, p.grid, sizeof(Shared) + words, s, a, p);
     if (e != hipSuccess || !p.split) return e;
     const int64_t rows = a.B * a.N * a.Hq;
-    k_attend_join<T, TR, KU><<<row_grid((rows + kWaves - 1) / kWaves, kThreads), kThreads, 0, s>>>(a, p);
+    if (rows <= kWideRows)
+        k_attend_join<T, TR, KU, true><<<(unsigned)rows, kThreads, 0, s>>>(a, p);
+    else
+        k_attend_join<T, TR, KU, false><<<row_grid((rows + kWaves - 1) / kWaves, kThreads), kThreads, 0, s>>>(a, p);
     return hipGetLastError();
 }
 
 template <class T, int DP>
 hipError_t attend_rows(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-    const Choice c = choose(a.N, a.Hq, a.Hk);
-    if (c.few)
-        return c.m == 1 ? attend_as<T, DP, 1, true>(a, p, s) : attend_as<T, DP, 2, true>(a, p, s);
-    return c.m == 1 ? attend_as<T, DP, 1, false>(a, p, s) : attend_as<T, DP, 2, false>(a, p, s);
+    const Choice c = choose(a.N, a.Hq, a.Hk, a.D);
+    if constexpr (DP <= 128)
+        if (c.m == 2)
+            return c.few ? attend_as<T, DP, 2, true>(a, p, s) : attend_as<T, DP, 2, false>(a, p, s);
+    return c.few ? attend_as<T, DP, 1, true>(a, p, s) : attend_as<T, DP, 1, false>(a, p, s);
 }
 
 template <class T>
 hipError_t attend_type(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
     if (a.D <= 64) return attend_rows<T, 64>(a, p, s);
-    if (a.D <= 96) return attend_rows<T, 96>(a, p, s);
     if (a.D <= 128) return attend_rows<T, 128>(a, p, s);
     return attend_rows<T, 256>(a, p, s);
 }
@@ -754,8 +918,8 @@ hipError_t attend_type(const AttendArgs& a, const AttendPlan& p, hipStream_t s) 
 size_t attend_workspace(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D) {
     return attend_plan(B, N, Hq, Hk, D, nullptr).bytes;
 }
-int64_t attend_grid(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t) {
-    const int64_t TR = choose(N, Hq, Hk).rows();
+int64_t attend_grid(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D) {
+    const int64_t TR = choose(N, Hq, Hk, D).rows();
     return B * Hk * ((N * (Hq / Hk) + TR - 1) / TR) + kWant + 8;
 }
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
