@@ -342,7 +342,21 @@ __device__ __forceinline__ void load_to_lds(const short* from, short* to) {
 }
 
 // Waits for the wave's loads to LDS (a barrier does not)
-__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void loads_done() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+    asm volatile("" ::: "memory");
+}
+
+// Operands are read from LDS this many products ahead, and the scheduler keeps to it: without that it
+// reads each where it is used, and its latency is all there is to see.
+template <int M>
+constexpr int kAheadOf = 8 / M;
+#define in_step(products, reads)                                      \
+    do {                                                              \
+        if (products) __builtin_amdgcn_sched_group_barrier(0x008, products, 0); \
+        __builtin_amdgcn_sched_group_barrier(0x100, reads, 0);        \
+    } while (0)
 
 // ---- a tile of slots against a wave's rows ----
 
@@ -355,7 +369,7 @@ __device__ __forceinline__ S8 query(const AttendArgs& a, const Work& w, int r, i
 
 template <class T, int DP, int M, int KT>
 struct RowsOf {
-    static constexpr int kPairs = KT / 32;
+    static constexpr int kPairs = KT / 32, kAhead = kAheadOf<M>;
     F4 o[M][DP / 16];
     float m[M], l[M];
 
@@ -373,16 +387,22 @@ struct RowsOf {
     __device__ __forceinline__ void scores(const short* K, const S8 (&q)[M][DP / 32], F4 (&s)[M][KT / 16]) {
         const int lane = threadIdx.x % kWave, row = lane % 16, quarter = lane / 16;
         const int swap = Tile<DP>::k_swap(row);   // (the same for row + 16)
+        constexpr int kEach = DP / 32, kAll = KT / 16 * kEach;
+        auto operand = [&](int i) {
+            return *(const S8*)(K + (i / kEach * 16 + row) * DP + ((i % kEach * 4 + quarter) ^ swap) * 8);
+        };
+        S8 f[kAhead];
 #pragma unroll
-        for (int t = 0; t < KT / 16; ++t) {
+        for (int i = 0; i < kAhead; ++i) f[i] = operand(i);
+        in_step(0, kAhead);
 #pragma unroll
-            for (int x = 0; x < M; ++x) s[x][t] = F4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < kAll; ++i) {
+            const int t = i / kEach;
 #pragma unroll
-            for (int k = 0; k < DP / 32; ++k) {
-                const S8 f = *(const S8*)(K + (t * 16 + row) * DP + ((k * 4 + quarter) ^ swap) * 8);
-#pragma unroll
-                for (int x = 0; x < M; ++x) s[x][t] = mma<T>(f, q[x][k], s[x][t]);
-            }
+            for (int x = 0; x < M; ++x)
+                s[x][t] = mma<T>(f[i % kAhead], q[x][i % kEach], i % kEach ? s[x][t] : F4{0.f, 0.f, 0.f, 0.f});
+            if (i + kAhead < kAll) f[i % kAhead] = operand(i + kAhead);
+            in_step(M, 1);
         }
     }
 
@@ -414,15 +434,20 @@ struct RowsOf {
 #pragma unroll
                 for (int t = 0; t < DP / 16; ++t) o[x][t] *= f;
             }
+#pragma unroll
+            for (int t = 0; t < KT / 16; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[x][t][e] = fmaf(s[x][t][e], c2, -m[x]);
+#pragma unroll
+            for (int t = 0; t < KT / 16; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[x][t][e] = exp2_(s[x][t][e]);
             float sum = 0.f;
 #pragma unroll
             for (int t = 0; t < KT / 16; ++t) {
+                sum += (s[x][t][0] + s[x][t][1]) + (s[x][t][2] + s[x][t][3]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float y = exp2_(fmaf(s[x][t][e], c2, -m[x]));
-                    sum += y;
-                    p[x][t / 2][t % 2 * 4 + e] = (short)from_f<T>(y).u;
-                }
+                for (int e = 0; e < 4; ++e) p[x][t / 2][t % 2 * 4 + e] = (short)from_f<T>(s[x][t][e]).u;
             }
             l[x] += sum;
         }
@@ -431,16 +456,24 @@ struct RowsOf {
     __device__ __forceinline__ void values(const short* V, const S8 (&p)[M][kPairs]) {
         const int lane = threadIdx.x % kWave, row = lane % 16, quarter = lane / 16;
         const int slot = quarter * 4 + row / 4, swap = Tile<DP>::v_swap(slot);   // (the same for slot + 16)
+        auto operand = [&](int i) {
+            const int t = i / kPairs, k = i % kPairs;
+            const short* at = V + (k * 32 + slot) * DP + ((t * 2 + row % 4 / 2) ^ swap) * 8 + row % 2 * 4;
+            const S4 lo = read_turned(at), hi = read_turned(at + 16 * DP);
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        constexpr int kAll = DP / 16 * kPairs;
+        S8 f[kAhead];
 #pragma unroll
-        for (int t = 0; t < DP / 16; ++t)
+        for (int i = 0; i < kAhead; ++i) f[i] = operand(i);
+        in_step(0, 2 * kAhead);
 #pragma unroll
-            for (int k = 0; k < kPairs; ++k) {
-                const short* at = V + (k * 32 + slot) * DP + ((t * 2 + row % 4 / 2) ^ swap) * 8 + row % 2 * 4;
-                const S4 lo = read_turned(at), hi = read_turned(at + 16 * DP);
-                const S8 f = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        for (int i = 0; i < kAll; ++i) {
 #pragma unroll
-                for (int x = 0; x < M; ++x) o[x][t] = mma<T>(f, p[x][k], o[x][t]);
-            }
+            for (int x = 0; x < M; ++x) o[x][i / kPairs] = mma<T>(f[i % kAhead], p[x][i % kPairs], o[x][i / kPairs]);
+            if (i + kAhead < kAll) f[i % kAhead] = operand(i + kAhead);
+            in_step(M, 2);
+        }
     }
 
     // The sums of a row's four lanes
