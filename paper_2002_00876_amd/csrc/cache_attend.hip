@@ -334,11 +334,16 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, int head, const P
 // 16 bytes a lane from `from` to LDS: those of the wave's lane l to `to` + 16 l, `to` the same in all.  The
 // load has no result that the compiler would wait for, which the builtin of it makes it do at the next read
 // of any LDS: loads_done() waits.  (M0 holds the LDS address and is read one state after it is written.)
+template <bool kOnce>
 __device__ __forceinline__ void load_to_lds(const short* from, short* to) {
     const uint32_t at = __builtin_amdgcn_readfirstlane(
         (uint32_t)(uintptr_t)(__attribute__((address_space(3))) short*)to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from)
-                 : "memory");
+    if constexpr (kOnce)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(at), "v"(from)
+                     : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from)
+                     : "memory");
 }
 
 // Waits for the wave's loads to LDS (a barrier does not)
@@ -583,13 +588,15 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a, Atten
         for (int y = 0; y < DP / 32; ++y) q[x][y] = query(a, w, first + x * 16 + lane % 16, y);
     auto ask = [&](int u) { return ask_page(a, pages, u * KT + tid % KT, end); };
     auto fetch = [&](int u) {
+        Place from[kPass];   // all of them first: LDS would be waited for before each load
+#pragma unroll
+        for (int i = 0; i < kPass; ++i) from[i] = sh.place[u % 3][(i * kThreads + tid) / kRow];
 #pragma unroll
         for (int i = 0; i < kPass; ++i) {
             const int x = i * kThreads + tid, slot = x / kRow, at = x % kRow;
-            const Place from = sh.place[u % 3][slot];
             const int to = (i * kThreads + wave * kWave) * 8;
-            load_to_lds(from.k + Tile<DP>::element(at ^ Tile<DP>::k_swap(slot), a.D), sh.k[u % 2] + to);
-            load_to_lds(from.v + Tile<DP>::element(at ^ Tile<DP>::v_swap(slot), a.D), sh.v[u % 2] + to);
+            load_to_lds<false>(from[i].k + Tile<DP>::element(at ^ Tile<DP>::k_swap(slot), a.D), sh.k[u % 2] + to);
+            load_to_lds<false>(from[i].v + Tile<DP>::element(at ^ Tile<DP>::v_swap(slot), a.D), sh.v[u % 2] + to);
         }
     };
     if (tid < KT) {
@@ -688,16 +695,18 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_few(AttendArgs a, Attend
             const short* from = sh.place[wave][u % 2][t * 16 + lane % 16].k;
 #pragma unroll
             for (int y = 0; y < DP / 32; ++y)
-                k[t][y] = *(const S8*)(from + Tile<DP>::element(y * 4 + lane / 16, a.D));
+                k[t][y] = __builtin_nontemporal_load((const S8*)(from + Tile<DP>::element(y * 4 + lane / 16, a.D)));
         }
     };
     auto fetch_values = [&](int u) {
+        const short* from[kPass];   // all of them first: LDS would be waited for before each load
+#pragma unroll
+        for (int i = 0; i < kPass; ++i) from[i] = sh.place[wave][u % 2][(i * kWave + lane) / kRow].v;
 #pragma unroll
         for (int i = 0; i < kPass; ++i) {
             const int x = i * kWave + lane, slot = x / kRow;
-            const short* from = sh.place[wave][u % 2][slot].v;
-            load_to_lds(from + Tile<DP>::element(x % kRow ^ Tile<DP>::v_swap(slot), a.D),
-                        sh.v[wave][u % 2] + i * kWave * 8);
+            load_to_lds<true>(from[i] + Tile<DP>::element(x % kRow ^ Tile<DP>::v_swap(slot), a.D),
+                              sh.v[wave][u % 2] + i * kWave * 8);
         }
     };
     keep(lo, ask(lo));
@@ -727,19 +736,17 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend_few(AttendArgs a, Attend
         if (u + 1 < hi) fetch_keys(u + 1);
         const Page next = ask(u + 2);
         apart();
-        if (at < end) {
-            S8 n[M][1];
-            if (at + KT > start) {
+        S8 n[M][1];
+        if (at + KT > start) {
 #pragma unroll
-                for (int x = 0; x < M; ++x) {
-                    const int r = min(w.tile * TR + x * 16 + lane % 16, w.s.rows - 1);
-                    R::mask(s[x], 0, seen(a, sh.words, r / (a.Hq / a.Hk), at, start, end));
-                }
+            for (int x = 0; x < M; ++x) {
+                const int r = min(w.tile * TR + x * 16 + lane % 16, w.s.rows - 1);
+                R::mask(s[x], 0, seen(a, sh.words, r / (a.Hq / a.Hk), at, start, end));
             }
-            rows.numerators(s, n, a.c2);
-            apart();
-            rows.values(sh.v[wave][u % 2], n);
         }
+        rows.numerators(s, n, a.c2);
+        apart();
+        rows.values(sh.v[wave][u % 2], n);
         keep(u + 2, next);
     }
     rows.finish();
