@@ -13,6 +13,8 @@
 //
 // Numerators are rounded to the cache's type for the product (their sum is not): each is off by half a
 // step at most, as the values are themselves, and the products are summed in 32 bits.
+#include <algorithm>
+
 #include "cache.h"
 #include "internal.h"
 
@@ -57,17 +59,20 @@ __device__ __forceinline__ S4 read_turned(const short* at) {
 
 // ---- how the slots are divided ----
 //
-// A unit is a row tile's walk over KU slots.  The units of all row tiles, one tile after the other, make a
-// line that is cut into equal stretches, one a workgroup, whatever the lengths: none of them waits for a
-// longer one.  What a workgroup has of a row tile is written as a part where the tile goes on elsewhere; a
-// stretch has two such ends at most.
+// A unit is a row tile's walk over KU slots of a key head.  A head's units of all row tiles, one tile after
+// the other, make a line that is cut into equal stretches, one a workgroup, whatever the lengths: none of
+// them waits for a longer one.  All heads' lines are cut alike and their stretches lie side by side, so that
+// the heads of a slot, which lie one behind the other in most caches, are read at about the same time (64
+// contexts of up to 8000 slots, 8 heads of 128: 184 us where each head had stretches of its own, and 169 so).
+// What a workgroup has of a row tile is written as a part where the tile goes on elsewhere; a stretch has two
+// such ends at most.
 struct AttendPlan {
     int tiles;          // row tiles of a key head, of N drafts
     int least;          // units of a stretch, at least
     bool split;         // otherwise a workgroup takes one row tile
     unsigned grid;
     int* per;           // workspace: units of a stretch
-    uint64_t* before;   // [B]: units of the sequences before
+    uint64_t* before;   // [B]: units of a head's sequences before
     float2* ml;         // [2 * grid][rows of a tile]: maximum (of exponents to base 2) and sum
     float* o;           // [2 * grid][rows of a tile][D]
     size_t bytes;
@@ -85,9 +90,6 @@ __device__ __forceinline__ int afresh(int x) {
     asm volatile("" : "+v"(x));
     return x;
 }
-
-// The scheduler mixes nothing from before with what comes after: their registers are not held together
-__device__ __forceinline__ void apart() { __builtin_amdgcn_sched_barrier(0); }
 
 struct Shape {
     int rows, units, tiles;   // of a sequence: rows, units of a row tile, row tiles of a key head
@@ -134,7 +136,7 @@ struct Walk {
     const AttendPlan& p;
     WalkShared& sh;
     uint64_t begin, at, end;   // of the workgroup's stretch
-    int per, g;
+    int per, stretch, head;
 
     // The stretch; every thread calls it
     __device__ __forceinline__ Walk(const AttendArgs& a_, const AttendPlan& p_, WalkShared& sh_)
@@ -142,9 +144,9 @@ struct Walk {
         const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
         if (!p.split) {
             const int total = (int)a.B * a.Hk * p.tiles, many = (total + 7) / 8;
-            g = (int)(blockIdx.x % 8) * many + (int)(blockIdx.x / 8);
+            stretch = (int)(blockIdx.x % 8) * many + (int)(blockIdx.x / 8);
             begin = at = 0;
-            end = (int)(blockIdx.x / 8) < many && g < total;
+            end = (int)(blockIdx.x / 8) < many && stretch < total;
             per = 1;
             return;
         }
@@ -156,7 +158,7 @@ struct Walk {
             mine[k] = 0;
             if (b < a.B) {
                 const Shape s = shape_of<TR, KU>(a, b);
-                mine[k] = (uint64_t)s.units * (s.tiles * a.Hk);
+                mine[k] = (uint64_t)s.units * s.tiles;
             }
             all += mine[k];
         }
@@ -182,12 +184,15 @@ struct Walk {
             start += mine[k];
         }
         total = uniform(total);
-        per = uniform(max(p.least, (int)min((total + gridDim.x - 1) / gridDim.x, (uint64_t)1 << 30)));
+        const int most = (int)(gridDim.x / (unsigned)a.Hk);
+        per = uniform(max(p.least, (int)min((total + most - 1) / most, (uint64_t)1 << 30)));
         if (blockIdx.x == 0 && tid == 0) *p.per = per;
         // workgroups of an XCD take neighbouring stretches: row tiles of the same slots share its L2
-        const int used = (int)((total + per - 1) / per), many = (used + 7) / 8;
-        g = (int)(blockIdx.x % 8) * many + (int)(blockIdx.x / 8);
-        begin = at = uniform(min((uint64_t)g * per, total));
+        const int used = (int)((total + per - 1) / per) * a.Hk, many = (used + 7) / 8;
+        const int g = (int)(blockIdx.x % 8) * many + (int)(blockIdx.x / 8);
+        stretch = g / a.Hk;
+        head = g % a.Hk;
+        begin = at = uniform(min((uint64_t)stretch * per, total));
         end = (int)(blockIdx.x / 8) < many ? uniform(min(at + per, total)) : at;
         __syncthreads();
     }
@@ -195,7 +200,7 @@ struct Walk {
     __device__ __forceinline__ bool next(Work* w) {
         if (at >= end) return false;
         if (!p.split) {
-            const int each = a.Hk * p.tiles, b = g / each, rest = g - b * each;
+            const int each = a.Hk * p.tiles, b = stretch / each, rest = stretch - b * each;
             w->of(a, b, shape_of<TR, KU>(a, b));
             w->head = rest / p.tiles;
             w->tile = rest % p.tiles;
@@ -218,9 +223,9 @@ struct Walk {
         const int tile = uniform((int)(in >> 32 ? in / (uint32_t)w->s.units : (uint32_t)in / (uint32_t)w->s.units));
         w->lo = (int)(in - (uint64_t)tile * w->s.units);
         w->hi = uniform((int)min((uint64_t)w->s.units, w->lo + (end - at)));
-        w->head = tile / w->s.tiles;
-        w->tile = tile % w->s.tiles;
-        w->part = w->lo == 0 && w->hi == w->s.units ? -1 : 2 * g + (at != begin);
+        w->head = head;
+        w->tile = tile;
+        w->part = w->lo == 0 && w->hi == w->s.units ? -1 : 2 * (stretch * a.Hk + head) + (at != begin);
         at += w->hi - w->lo;
         return true;
     }
@@ -314,42 +319,39 @@ struct __attribute__((aligned(16))) Place {
     const short* k;
     const short* v;
 };
-// A slot's page is asked for while a tile is worked on, and its place made of it afterwards
-struct Page {
-    int id, at;
-    bool there;
-};
-__device__ __forceinline__ Page ask_page(const AttendArgs& a, const int32_t* pages, int j, int end) {
-    Page x;
-    x.there = j < end;
-    x.id = pages[page_of(a.c, min(j, end - 1), &x.at)];
-    return x;
-}
-__device__ __forceinline__ Place place_of(const AttendArgs& a, int head, const Page& x) {
-    const int64_t off = x.there ? token_offset(a.c, x.id, x.at) : -1, at = off + (int64_t)head * a.c.sh;
+__device__ __forceinline__ Place place_of(const AttendArgs& a, int head, int id, int token, bool there) {
+    const int64_t off = there ? token_offset(a.c, id, token) : -1, at = off + (int64_t)head * a.c.sh;
     return off < 0 ? Place{(const short*)kZeros, (const short*)kZeros}
                    : Place{(const short*)a.c.k + at, (const short*)a.c.v + at};
 }
 
-// 16 bytes a lane from `from` to LDS: those of the wave's lane l to `to` + 16 l, `to` the same in all.  The
-// load has no result that the compiler would wait for, which the builtin of it makes it do at the next read
-// of any LDS: loads_done() waits.  (M0 holds the LDS address and is read one state after it is written.)
-template <bool kOnce>
-__device__ __forceinline__ void load_to_lds(const short* from, short* to) {
-    const uint32_t at = __builtin_amdgcn_readfirstlane(
-        (uint32_t)(uintptr_t)(__attribute__((address_space(3))) short*)to);
-    if constexpr (kOnce)
+// 16 bytes a lane from `from` to LDS: those of the wave's lane l to `to` + 16 l, `to` the same in all.  once:
+// nothing else will read them, so they are not kept in the caches.  The load has no result that the compiler
+// would wait for, which its builtin makes it do at the next read of any LDS: loads_done() waits.  (M0 holds
+// the LDS address and is read one state after it is written; nothing else here uses it.)
+__device__ __forceinline__ uint32_t lds_address(const void* at) {
+    return (uint32_t)uniform((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)at);
+}
+__device__ __forceinline__ void load_to_lds(const short* from, short* to, bool once) {
+    const uint32_t at = lds_address(to);
+    if (once)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(at), "v"(from)
                      : "memory");
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from)
                      : "memory");
 }
+// 4 bytes a lane, likewise
+__device__ __forceinline__ void load_id_to_lds(const int32_t* from, int32_t* to) {
+    const uint32_t at = lds_address(to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(at), "v"(from) : "memory");
+}
 
-// Waits for the wave's loads to LDS (a barrier does not)
+// Waits until at most `left` of the wave's loads are on their way (a barrier does not)
+template <int left>
 __device__ __forceinline__ void loads_done() {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (left & 15) | (left >> 4) << 14);   // vmcnt
     asm volatile("" ::: "memory");
 }
 
@@ -543,239 +545,131 @@ __device__ void store_padding(const AttendArgs& a, const Work& w) {
             .store(i % each * 4, F4{0.f, 0.f, 0.f, 0.f});
 }
 
-// ---- many rows: a wave takes M * 16 of them, all share the tile of slots ----
+// ---- the kernel ----
 
-template <int DP>
-constexpr int kTile = DP > 128 ? 32 : 64;
+// Slots of a unit, and tiles in LDS: one is worked on and the others are on their way.
+template <int DP, int M>
+constexpr int kSlots = DP == 64 || M == 2 ? 64 : 32;
+template <int DP, int M>
+constexpr int kStages = M == 2 || DP == 256 ? 2 : 4;
 
-template <class T, int DP, int M>
-struct ManyShared {
-    static constexpr int KT = kTile<DP>;
-    using R = RowsOf<T, DP, M, KT>;
-    short k[2][KT * DP];
-    short v[2][KT * DP];
-    Place place[3][KT];
+template <int DP, int KT, int NS>
+struct AttendShared {
+    short k[NS][KT * DP];
+    short v[NS][KT * DP];
+    Place place[NS][KT];
+    int32_t ids[NS][KT];
     WalkShared walk;
     short up[kMaxNodes];
     uint32_t words[];   // [N][ceil(N / 32)], where there are parents
 };
 
+// A wave takes 16 * M of a tile's rows, and all take each tile of slots.
 template <class T, int DP, int M>
-__global__ __launch_bounds__(kThreads, 2) void k_attend_many(AttendArgs a, AttendPlan p) {
-    using Shared = ManyShared<T, DP, M>;
-    using R = typename Shared::R;
-    constexpr int KT = Shared::KT, TR = 16 * M * kWaves, kRow = DP / 8, kPass = KT * kRow / kThreads;
+__global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan p) {
+    constexpr int KT = kSlots<DP, M>, NS = kStages<DP, M>, kFar = NS - 1;
+    constexpr int TR = 16 * M * kWaves, kRow = DP / 8, kPass = KT * kRow / kThreads;
+    using Shared = AttendShared<DP, KT, NS>;
+    using R = RowsOf<T, DP, M, KT>;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Shared& sh = *(Shared*)lds;
     const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave);
     Walk<TR, KT> walk(a, p, sh.walk);
     Work w;
     while (walk.next(&w)) {
-    if (w.tile >= w.s.tiles) {
-        store_padding<T, TR>(a, w);
-        return;   // there is nothing behind it
-    }
-    const int n = w.n, start = w.start, end = w.end, lo = w.lo, hi = w.hi;
-    if (a.parents && (int64_t)hi * KT > start) find_ancestors(a, w.b, n, sh.words, sh.up);
-    const int32_t* pages = a.c.pages + w.b * a.c.M;
-    const int first = w.tile * TR + wave * 16 * M;
-    R rows;
-    rows.init();
-    S8 q[M][DP / 32];
-#pragma unroll
-    for (int x = 0; x < M; ++x)
-#pragma unroll
-        for (int y = 0; y < DP / 32; ++y) q[x][y] = query(a, w, first + x * 16 + lane % 16, y);
-    auto ask = [&](int u) { return ask_page(a, pages, u * KT + tid % KT, end); };
-    auto fetch = [&](int u) {
-        Place from[kPass];   // all of them first: LDS would be waited for before each load
-#pragma unroll
-        for (int i = 0; i < kPass; ++i) from[i] = sh.place[u % 3][(i * kThreads + tid) / kRow];
-#pragma unroll
-        for (int i = 0; i < kPass; ++i) {
-            const int x = i * kThreads + tid, slot = x / kRow, at = x % kRow;
-            const int to = (i * kThreads + wave * kWave) * 8;
-            load_to_lds<false>(from[i].k + Tile<DP>::element(at ^ Tile<DP>::k_swap(slot), a.D), sh.k[u % 2] + to);
-            load_to_lds<false>(from[i].v + Tile<DP>::element(at ^ Tile<DP>::v_swap(slot), a.D), sh.v[u % 2] + to);
+        if (w.tile >= w.s.tiles) {
+            store_padding<T, TR>(a, w);
+            return;   // there is nothing behind it
         }
-    };
-    if (tid < KT) {
-        sh.place[lo % 3][tid] = place_of(a, w.head, ask(lo));
-        sh.place[(lo + 1) % 3][tid] = place_of(a, w.head, ask(lo + 1));
-    }
-    __syncthreads();
-    fetch(lo);
-    for (int u = lo; u < hi; ++u) {
-        const short *ks = sh.k[u % 2], *vs = sh.v[u % 2];
-        loads_done();
-        __syncthreads();
-        if (u + 1 < hi) fetch(u + 1);
-        const Page next = ask(u + 2);
-        F4 s[M][KT / 16];
-        S8 n[M][R::kPairs];
-        rows.scores(ks, q, s);
-        if ((u + 1) * KT > start) {
+        const int lo = w.lo, hi = w.hi, first = w.tile * TR + wave * 16 * M, G = a.Hq / a.Hk;
+        const int32_t* pages = a.c.pages + w.b * a.c.M;
+        // Page numbers go to LDS, too, by the first wave, kFar units before they are made places of: the
+        // compiler would wait for all loads before it if one of them had a result.
+        auto ask = [&](int u) {
+            int at;
+            const int page = page_of(a.c, min(u * KT + lane, w.end - 1), &at);
+            if (lane < KT) load_id_to_lds(pages + page, sh.ids[u % NS]);
+        };
+        auto find = [&](int u) {
+            const int j = u * KT + lane;
+            int at;
+            page_of(a.c, min(j, w.end - 1), &at);
+            if (lane < KT) sh.place[u % NS][lane] = place_of(a, w.head, sh.ids[u % NS][lane], at, j < w.end);
+        };
+        auto fetch = [&](int u) {
+            Place from[kPass];   // all of them first: LDS would be waited for before each load
 #pragma unroll
-            for (int x = 0; x < M; ++x) {
-                const int i = min(first + x * 16 + lane % 16, w.s.rows - 1) / (a.Hq / a.Hk);
+            for (int i = 0; i < kPass; ++i) from[i] = sh.place[u % NS][(i * kThreads + tid) / kRow];
 #pragma unroll
-                for (int y = 0; y < R::kPairs; ++y)
-                    R::mask(s[x], y, seen(a, sh.words, i, u * KT + y * 32, start, end));
+            for (int i = 0; i < kPass; ++i) {
+                const int x = i * kThreads + tid, slot = x / kRow, at = x % kRow;
+                const int to = (i * kThreads + wave * kWave) * 8;
+                const short* k = from[i].k + Tile<DP>::element(at ^ Tile<DP>::k_swap(slot), a.D);
+                const short* v = from[i].v + Tile<DP>::element(at ^ Tile<DP>::v_swap(slot), a.D);
+                load_to_lds(k, sh.k[u % NS] + to, p.tiles == 1);
+                load_to_lds(v, sh.v[u % NS] + to, p.tiles == 1);
             }
+        };
+        for (int x = tid; x < NS * KT; x += kThreads) {
+            const int u = lo + x / KT, j = u * KT + x % KT;
+            int at;
+            const int page = page_of(a.c, min(j, w.end - 1), &at);
+            sh.place[u % NS][x % KT] = place_of(a, w.head, pages[page], at, j < w.end);
         }
-        rows.numerators(s, n, a.c2);
-        rows.values(vs, n);
-        if (tid < KT) sh.place[(u + 2) % 3][tid] = place_of(a, w.head, next);
-    }
-    rows.finish();
-    const int own = afresh(lane);
-#pragma unroll
-    for (int x = 0; x < M; ++x) {
-        const Target<T, TR> to(a, p, w, wave * 16 * M + x * 16 + own % 16, rows.m[x], rows.l[x], own < 16);
-#pragma unroll
-        for (int t = 0; t < DP / 16; ++t) {
-            const int d = t * 16 + own / 16 * 4;
-            if (d < a.D) to.store(d, rows.o[x][t]);
-        }
-    }
-    __syncthreads();   // the tiles are free for the next stretch of a row tile
-    }
-}
-
-// ---- few rows: every wave takes all of them, and slots of its own ----
-
-template <class T, int DP, int M>
-struct FewShared {
-    static constexpr int KT = 32;
-    using R = RowsOf<T, DP, M, KT>;
-    union {
-        short v[kWaves][2][KT * DP];
-        float o[kWaves][M * 16][DP];
-    };
-    Place place[kWaves][2][KT];
-    float2 ml[kWaves][M * 16];
-    S8 q[M * (DP / 32)][kWave];   // the queries' operand, in the order of the lanes that use it
-    WalkShared walk;
-    short up[M * 16];
-    uint32_t words[];
-};
-
-template <class T, int DP, int M>
-__global__ __launch_bounds__(kThreads, 2) void k_attend_few(AttendArgs a, AttendPlan p) {
-    using Shared = FewShared<T, DP, M>;
-    using R = typename Shared::R;
-    constexpr int KT = Shared::KT, KU = KT * kWaves, TR = 16 * M, kRow = DP / 8, kPass = KT * kRow / kWave;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    Shared& sh = *(Shared*)lds;
-    const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave);
-    Walk<TR, KU> walk(a, p, sh.walk);
-    Work w;
-    while (walk.next(&w)) {
-    if (w.tile >= w.s.tiles) {
-        store_padding<T, TR>(a, w);
-        return;   // there is nothing behind it
-    }
-    const int n = w.n, start = w.start, end = w.end, lo = w.lo, hi = w.hi;
-    if (a.parents && (int64_t)hi * KU > start) find_ancestors(a, w.b, n, sh.words, sh.up);
-    const int32_t* pages = a.c.pages + w.b * a.c.M;
-    R rows;
-    rows.init();
-    for (int x = wave; x < M * (DP / 32); x += kWaves)
-        sh.q[x][lane] = query(a, w, w.tile * TR + x / (DP / 32) * 16 + lane % 16, x % (DP / 32));
-    // the places of the wave's own slots of unit u
-    auto ask = [&](int u) { return ask_page(a, pages, u * KU + wave * KT + lane % KT, end); };
-    auto keep = [&](int u, const Page& x) {
-        if (lane < KT) sh.place[wave][u % 2][lane] = place_of(a, w.head, x);
-    };
-    // Keys go to registers, as a wave's own operand, values to LDS, where they are turned
-    S8 k[KT / 16][DP / 32];
-    auto fetch_keys = [&](int u) {
-#pragma unroll
-        for (int t = 0; t < KT / 16; ++t) {
-            const short* from = sh.place[wave][u % 2][t * 16 + lane % 16].k;
-#pragma unroll
-            for (int y = 0; y < DP / 32; ++y)
-                k[t][y] = __builtin_nontemporal_load((const S8*)(from + Tile<DP>::element(y * 4 + lane / 16, a.D)));
-        }
-    };
-    auto fetch_values = [&](int u) {
-        const short* from[kPass];   // all of them first: LDS would be waited for before each load
-#pragma unroll
-        for (int i = 0; i < kPass; ++i) from[i] = sh.place[wave][u % 2][(i * kWave + lane) / kRow].v;
-#pragma unroll
-        for (int i = 0; i < kPass; ++i) {
-            const int x = i * kWave + lane, slot = x / kRow;
-            load_to_lds<true>(from[i] + Tile<DP>::element(x % kRow ^ Tile<DP>::v_swap(slot), a.D),
-                              sh.v[wave][u % 2] + i * kWave * 8);
-        }
-    };
-    keep(lo, ask(lo));
-    fetch_values(lo);
-    fetch_keys(lo);
-    keep(lo + 1, ask(lo + 1));
-    __syncthreads();   // the queries are there
-    for (int u = lo; u < hi; ++u) {
-        loads_done();
-        if (u + 1 < hi) fetch_values(u + 1);
-        apart();
-        const int at = u * KU + wave * KT;
-        F4 s[M][KT / 16];
+        S8 q[M][DP / 32];
 #pragma unroll
         for (int x = 0; x < M; ++x)
 #pragma unroll
-            for (int t = 0; t < KT / 16; ++t) s[x][t] = F4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int y = 0; y < DP / 32; ++y)
-#pragma unroll
-            for (int x = 0; x < M; ++x) {
-                const S8 q = sh.q[x * (DP / 32) + y][lane];
-#pragma unroll
-                for (int t = 0; t < KT / 16; ++t) s[x][t] = mma<T>(k[t][y], q, s[x][t]);
+            for (int y = 0; y < DP / 32; ++y) q[x][y] = query(a, w, first + x * 16 + lane % 16, y);
+        if (a.parents && hi * KT > w.start) find_ancestors(a, w.b, w.n, sh.words, sh.up);
+        loads_done<0>();   // (what has results)
+        __syncthreads();
+        if (wave == 0)
+            for (int u = lo + NS; u < lo + NS + kFar; ++u) ask(u);
+        for (int u = lo; u < min(lo + kFar, hi); ++u) fetch(u);
+        R rows;
+        rows.init();
+        for (int u = lo; u < hi; ++u) {
+            // loads come back in order: all but those of the units behind this one are there
+            if (u + kFar <= hi)
+                loads_done<(kFar - 1) * 2 * kPass>();
+            else
+                loads_done<0>();
+            __syncthreads();
+            if (u + kFar < hi) fetch(u + kFar);
+            if (wave == 0) {
+                ask(u + NS + kFar);
+                find(u + NS);
             }
-        apart();
-        if (u + 1 < hi) fetch_keys(u + 1);
-        const Page next = ask(u + 2);
-        apart();
-        S8 n[M][1];
-        if (at + KT > start) {
+            if (first >= w.s.rows) continue;
+            F4 s[M][KT / 16];
+            S8 n[M][R::kPairs];
+            rows.scores(sh.k[u % NS], q, s);
+            if ((u + 1) * KT > w.start) {
 #pragma unroll
-            for (int x = 0; x < M; ++x) {
-                const int r = min(w.tile * TR + x * 16 + lane % 16, w.s.rows - 1);
-                R::mask(s[x], 0, seen(a, sh.words, r / (a.Hq / a.Hk), at, start, end));
+                for (int x = 0; x < M; ++x) {
+                    const int i = min(first + x * 16 + lane % 16, w.s.rows - 1) / G;
+#pragma unroll
+                    for (int y = 0; y < R::kPairs; ++y)
+                        R::mask(s[x], y, seen(a, sh.words, i, u * KT + y * 32, w.start, w.end));
+                }
+            }
+            rows.numerators(s, n, a.c2);
+            rows.values(sh.v[u % NS], n);
+        }
+        rows.finish();
+        const int own = afresh(lane);
+#pragma unroll
+        for (int x = 0; x < M; ++x) {
+            const Target<T, TR> to(a, p, w, wave * 16 * M + x * 16 + own % 16, rows.m[x], rows.l[x], own < 16);
+#pragma unroll
+            for (int t = 0; t < DP / 16; ++t) {
+                const int d = t * 16 + own / 16 * 4;
+                if (d < a.D) to.store(d, rows.o[x][t]);
             }
         }
-        rows.numerators(s, n, a.c2);
-        apart();
-        rows.values(sh.v[wave][u % 2], n);
-        keep(u + 2, next);
-    }
-    rows.finish();
-    __syncthreads();   // the tiles make room for the waves' sums
-    const int own = afresh(lane);
-#pragma unroll
-    for (int x = 0; x < M; ++x) {
-        const int r = x * 16 + own % 16;
-#pragma unroll
-        for (int t = 0; t < DP / 16; ++t) *(F4*)&sh.o[wave][r][t * 16 + own / 16 * 4] = rows.o[x][t];
-        if (own < 16) sh.ml[wave][r] = make_float2(rows.m[x], rows.l[x]);
-    }
-    __syncthreads();
-    const int each = a.D / 4;
-    for (int i = afresh(tid); i < TR * each; i += kThreads) {
-        const int r = i / each, d = i % each * 4;
-        float m = kNone, l = 0.f;
-        F4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int y = 0; y < kWaves; ++y) m = fmaxf(m, sh.ml[y][r].x);
-#pragma unroll
-        for (int y = 0; y < kWaves; ++y) {
-            const float f = exp2_(sh.ml[y][r].x - m);
-            l += f * sh.ml[y][r].y;
-            o += f * *(const F4*)&sh.o[y][r][d];
-        }
-        Target<T, TR>(a, p, w, r, m, l, d == 0).store(d, o);
-    }
-    __syncthreads();   // the sums' places are free for the next stretch of a row tile
+        loads_done<0>();   // (page numbers)
+        __syncthreads();   // LDS is free for the next row tile
     }
 }
 
@@ -805,17 +699,17 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, AttendPl
         const int at = i * G + h % G, tile = at / TR;
         int pieces = 0, first = 0, begun = 0;
         if (tile < s.tiles) {   // (others are padding)
-            const uint64_t from = p.before[b] + (uint64_t)((h / G) * s.tiles + tile) * s.units;
-            const uint32_t g = over(from, per);
+            const uint64_t from = p.before[b] + (uint64_t)tile * s.units;
+            const uint32_t g = over(from, per);   // the first stretch that has some of the tile
             pieces = (int)(over(from + s.units - 1, per) - g) + 1;
             if (pieces == 1) continue;   // written as a whole
             if (at >= s.rows) pieces = 0;
             // the row tile's part of the first stretch is that stretch's second, unless both begin together
-            first = 2 * (int)g;
+            first = 2 * ((int)g * a.Hk + h / G);
             begun = (uint64_t)g * per != from;
         }
         const int lane_d = d < a.D ? d : 0;
-        auto row_of_part = [&](int y) { return (int64_t)(first + 2 * y + (y == 0 ? begun : 0)) * TR + at % TR; };
+        auto row_of_part = [&](int y) { return (int64_t)(first + 2 * a.Hk * y + (y == 0 ? begun : 0)) * TR + at % TR; };
         float m = kNone;
         for (int y = lane; y < pieces; y += kTeam) m = fmaxf(m, p.ml[row_of_part(y)].x);
         m = wave_max_fast(m);
@@ -867,29 +761,18 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, AttendPl
 
 // ---- launches ----
 
-// Rows of a tile and slots of a unit of the kernel that a call takes
-struct Choice {
-    int few, m;
-    int rows() const { return 16 * m * (few ? 1 : kWaves); }
-};
-Choice choose(int64_t N, int64_t Hq, int64_t Hk, int64_t D) {
-    const int64_t rows = N * (Hq / Hk);
-    if (D > 128) return {rows <= 16, 1};   // wider heads leave no registers for a second row a lane
-    if (rows <= 16) return {1, 1};
-    if (rows <= 32) return {1, 2};
-    if (rows <= 64) return {0, 1};
-    return {0, 2};
-}
+// Row tiles of 64 or 128 rows.  (Heads of more than 128 elements leave no registers for a second row a lane.)
+int sixteens(int64_t N, int64_t Hq, int64_t Hk, int64_t D) { return N * (Hq / Hk) > 64 && D <= 128 ? 2 : 1; }
 
 AttendPlan attend_plan(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D, void* ws) {
-    const Choice c = choose(N, Hq, Hk, D);
-    const int64_t TR = c.rows();
+    const int64_t TR = 16 * kWaves * sixteens(N, Hq, Hk, D);
     AttendPlan p{};
     p.tiles = (int)((N * (Hq / Hk) + TR - 1) / TR);
     p.split = B <= kSplitBatch;
-    p.least = c.few ? 1 : 2;
+    p.least = 2;
     const int64_t items = B * Hk * p.tiles;
-    p.grid = (unsigned)(p.split ? kWant : (items + 7) / 8 * 8);
+    // (a multiple of 8 of them, as each XCD takes an eighth)
+    p.grid = (unsigned)(p.split ? (std::max(kWant / Hk, (int64_t)1) * Hk + 7) / 8 * 8 : (items + 7) / 8 * 8);
     size_t off = 0;
     auto take = [&](size_t bytes) {
         char* at = (char*)ws + off;
@@ -916,34 +799,28 @@ hipError_t launch_lds(AllowLds& allow, size_t most, K kernel, unsigned grid, siz
     return hipGetLastError();
 }
 
-template <class T, int DP, int M, bool kFew>
+template <class T, int DP, int M>
 hipError_t attend_as(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-    using Shared = std::conditional_t<kFew, FewShared<T, DP, M>, ManyShared<T, DP, M>>;
-    constexpr int TR = 16 * M * (kFew ? 1 : kWaves), KU = kFew ? 32 * kWaves : kTile<DP>;
+    constexpr int TR = 16 * M * kWaves, KT = kSlots<DP, M>;
+    using Shared = AttendShared<DP, KT, kStages<DP, M>>;
     static AllowLds allow;
     const size_t words = a.parents ? (size_t)a.N * ((a.N + 31) / 32) * sizeof(uint32_t) : 0;
     const size_t most = sizeof(Shared) + (size_t)kMaxNodes * kWords * sizeof(uint32_t);
-    hipError_t e;
-    if constexpr (kFew)
-        e = launch_lds(allow, most, k_attend_few<T, DP, M>, p.grid, sizeof(Shared) + words, s, a, p);
-    else
-        e = launch_lds(allow, most, k_attend_many<T, DP, M>, p.grid, sizeof(Shared) + words, s, a, p);
+    const hipError_t e = launch_lds(allow, most, k_attend<T, DP, M>, p.grid, sizeof(Shared) + words, s, a, p);
     if (e != hipSuccess || !p.split) return e;
     const int64_t rows = a.B * a.N * a.Hq;
     if (rows <= kWideRows)
-        k_attend_join<T, TR, KU, true><<<(unsigned)rows, kThreads, 0, s>>>(a, p);
+        k_attend_join<T, TR, KT, true><<<(unsigned)rows, kThreads, 0, s>>>(a, p);
     else
-        k_attend_join<T, TR, KU, false><<<row_grid((rows + kWaves - 1) / kWaves, kThreads), kThreads, 0, s>>>(a, p);
+        k_attend_join<T, TR, KT, false><<<row_grid((rows + kWaves - 1) / kWaves, kThreads), kThreads, 0, s>>>(a, p);
     return hipGetLastError();
 }
 
 template <class T, int DP>
 hipError_t attend_rows(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-    const Choice c = choose(a.N, a.Hq, a.Hk, a.D);
     if constexpr (DP <= 128)
-        if (c.m == 2)
-            return c.few ? attend_as<T, DP, 2, true>(a, p, s) : attend_as<T, DP, 2, false>(a, p, s);
-    return c.few ? attend_as<T, DP, 1, true>(a, p, s) : attend_as<T, DP, 1, false>(a, p, s);
+        if (sixteens(a.N, a.Hq, a.Hk, a.D) == 2) return attend_as<T, DP, 2>(a, p, s);
+    return attend_as<T, DP, 1>(a, p, s);
 }
 
 template <class T>
@@ -959,7 +836,7 @@ size_t attend_workspace(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D)
     return attend_plan(B, N, Hq, Hk, D, nullptr).bytes;
 }
 int64_t attend_grid(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D) {
-    const int64_t TR = choose(N, Hq, Hk, D).rows();
+    const int64_t TR = 16 * kWaves * sixteens(N, Hq, Hk, D);
     return B * Hk * ((N * (Hq / Hk) + TR - 1) / TR) + kWant + 8;
 }
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
