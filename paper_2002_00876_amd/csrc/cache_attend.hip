@@ -549,9 +549,9 @@ __device__ void store_padding(const AttendArgs& a, const Work& w) {
 
 // Slots of a unit, and tiles in LDS: one is worked on and the others are on their way.
 template <int DP, int M>
-constexpr int kSlots = DP == 64 || M == 2 ? 64 : 32;
+constexpr int kSlots = DP == 256 ? 32 : 64;
 template <int DP, int M>
-constexpr int kStages = M == 2 || DP == 256 ? 2 : 4;
+constexpr int kStages = DP == 64 ? 4 : 2;
 
 template <int DP, int KT, int NS>
 struct AttendShared {
@@ -679,84 +679,125 @@ __device__ __forceinline__ uint32_t over(uint64_t x, int per) {   // (64-bit div
     return x >> 32 ? (uint32_t)(x / (uint32_t)per) : (uint32_t)x / (uint32_t)per;
 }
 
-// A team a row: its lanes' groups take every so many of the row's parts, each lane four elements of it.  A
-// team is a wave, or where rows are few and so in many parts a workgroup.
-template <class T, int TR, int KU, bool kWide>
+// Which parts make up a row tile's rows; pieces = 1: none, it was written as a whole
+template <int TR, int KU>
+struct Parts {
+    int pieces, first, begun, step, rows;
+
+    __device__ __forceinline__ Parts(const AttendArgs& a, const AttendPlan& p, int64_t b, int head, int tile) {
+        const int per = *p.per;
+        const Shape s = shape_of<TR, KU>(a, b);
+        pieces = first = begun = 0;
+        step = 2 * a.Hk;
+        rows = s.rows - tile * TR;
+        if (tile >= s.tiles) return;   // padding
+        const uint64_t from = p.before[b] + (uint64_t)tile * s.units;
+        const uint32_t g = over(from, per);   // the first stretch that has some of the tile
+        pieces = (int)(over(from + s.units - 1, per) - g) + 1;
+        // the tile's part of the first stretch is that stretch's second, unless both begin together
+        first = 2 * ((int)g * a.Hk + head);
+        begun = (uint64_t)g * per != from;
+    }
+    // Row r of part y
+    __device__ __forceinline__ int64_t row(int y, int r) const {
+        return (int64_t)(first + step * y + (y == 0 ? begun : 0)) * TR + r;
+    }
+};
+
+// Adds up a row's parts mine, mine + groups, ...: four elements a lane, from d on
+template <class P>
+__device__ __forceinline__ void add_parts(const AttendArgs& a, const AttendPlan& p, const P& parts, int r, int d,
+                                          int mine, int groups, int pieces, float m, F4* o, float* l) {
+    constexpr int kU = 4;   // parts asked for at once
+    for (int y = mine; y < pieces; y += kU * groups) {
+        float2 ml[kU];
+        F4 x[kU];
+#pragma unroll
+        for (int k = 0; k < kU; ++k) {
+            const int64_t z = parts.row(min(y + k * groups, pieces - 1), r);
+            ml[k] = p.ml[z];
+            x[k] = *(const F4*)(p.o + z * a.D + d);
+        }
+#pragma unroll
+        for (int k = 0; k < kU; ++k) {
+            const float f = y + k * groups < pieces ? exp2_(ml[k].x - m) : 0.f;
+            *l += f * ml[k].y;
+            *o += f * x[k];
+        }
+    }
+}
+
+// Lanes that have four elements of a row each
+__device__ __forceinline__ int lanes_across(int D) { return D <= 64 ? 16 : D <= 128 ? 32 : 64; }
+
+constexpr int kJoinRows = 16;
+
+// Many rows, of few parts each: a workgroup takes kJoinRows rows of a tile, a group of lanes a row
+template <class T, int TR, int KU>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, AttendPlan p) {
-    constexpr int kTeam = kWide ? kThreads : kWave;
+    const int G = a.Hq / a.Hk, across = lanes_across(a.D), d = (int)threadIdx.x % across * 4;
+    uint32_t at = blockIdx.x;
+    const int chunk = (int)(at % (TR / kJoinRows));
+    at /= TR / kJoinRows;
+    const int tile = (int)(at % (uint32_t)p.tiles);
+    at /= (uint32_t)p.tiles;
+    const int head = (int)(at % (uint32_t)a.Hk);
+    const int64_t b = at / (uint32_t)a.Hk;
+    const Parts<TR, KU> parts(a, p, b, head, tile);
+    if (parts.pieces == 1) return;
+    for (int r = chunk * kJoinRows + (int)threadIdx.x / across; r < (chunk + 1) * kJoinRows;
+         r += kThreads / across) {
+        const int in = tile * TR + r;
+        if (in >= a.N * G) return;
+        const int pieces = r < parts.rows ? parts.pieces : 0;
+        float m = kNone, l = 0.f;
+        for (int y = 0; y < pieces; ++y) m = fmaxf(m, p.ml[parts.row(y, r)].x);
+        F4 o = {0.f, 0.f, 0.f, 0.f};
+        add_parts(a, p, parts, r, d < a.D ? d : 0, 0, 1, pieces, m, &o, &l);
+        const int64_t row = (b * a.N + in / G) * a.Hq + head * G + in % G;
+        if (d < a.D) store4<T>((T*)a.out + row * a.D + d, o * (l > 0.f ? 1.f / l : 0.f));
+        if (d == 0 && a.lse) a.lse[row] = lse_of(m, l);
+    }
+}
+
+// Few rows, which may be in many parts: a workgroup a row, whose groups of lanes take every so many parts
+template <class T, int TR, int KU>
+__global__ __launch_bounds__(kThreads) void k_attend_join_wide(AttendArgs a, AttendPlan p) {
     __shared__ float tops[kWaves];
     __shared__ F4 sums[kWaves][kWave];
     __shared__ float weights[kWaves][kWave];
-    const int lane = threadIdx.x % kTeam, wave = threadIdx.x / kWave, G = a.Hq / a.Hk;
-    const int across = a.D <= 64 ? 16 : a.D <= 128 ? 32 : 64;   // lanes of a group
-    const int groups = kTeam / across, mine = lane / across, d = lane % across * 4;
-    const int64_t rows = a.B * a.N * a.Hq, step = (int64_t)gridDim.x * (kThreads / kTeam);
-    const int per = *p.per;
-    for (int64_t row = (int64_t)blockIdx.x * (kThreads / kTeam) + (kWide ? 0 : wave); row < rows; row += step) {
-        const int64_t b = row / ((int64_t)a.N * a.Hq);
-        const int rest = (int)(row - b * a.N * a.Hq), i = rest / a.Hq, h = rest % a.Hq;
-        const Shape s = shape_of<TR, KU>(a, b);
-        const int at = i * G + h % G, tile = at / TR;
-        int pieces = 0, first = 0, begun = 0;
-        if (tile < s.tiles) {   // (others are padding)
-            const uint64_t from = p.before[b] + (uint64_t)tile * s.units;
-            const uint32_t g = over(from, per);   // the first stretch that has some of the tile
-            pieces = (int)(over(from + s.units - 1, per) - g) + 1;
-            if (pieces == 1) continue;   // written as a whole
-            if (at >= s.rows) pieces = 0;
-            // the row tile's part of the first stretch is that stretch's second, unless both begin together
-            first = 2 * ((int)g * a.Hk + h / G);
-            begun = (uint64_t)g * per != from;
-        }
-        const int lane_d = d < a.D ? d : 0;
-        auto row_of_part = [&](int y) { return (int64_t)(first + 2 * a.Hk * y + (y == 0 ? begun : 0)) * TR + at % TR; };
-        float m = kNone;
-        for (int y = lane; y < pieces; y += kTeam) m = fmaxf(m, p.ml[row_of_part(y)].x);
-        m = wave_max_fast(m);
-        if constexpr (kWide) {
-            if (threadIdx.x % kWave == 0) tops[wave] = m;
-            __syncthreads();
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, G = a.Hq / a.Hk;
+    const int across = lanes_across(a.D), d = tid % across * 4;
+    const uint32_t row = blockIdx.x, each = (uint32_t)(a.N * a.Hq);
+    const int64_t b = row / each;
+    const int rest = (int)(row % each), i = rest / a.Hq, h = rest % a.Hq;
+    const int in = i * G + h % G, r = in % TR;
+    const Parts<TR, KU> parts(a, p, b, h / G, in / TR);
+    if (parts.pieces == 1) return;
+    const int pieces = r < parts.rows ? parts.pieces : 0;
+    float m = kNone, l = 0.f;
+    for (int y = tid; y < pieces; y += kThreads) m = fmaxf(m, p.ml[parts.row(y, r)].x);
+    m = wave_max_fast(m);
+    if (lane == 0) tops[wave] = m;
+    __syncthreads();
 #pragma unroll
-            for (int k = 0; k < kWaves; ++k) m = fmaxf(m, tops[k]);
-        }
-        float l = 0.f;
-        F4 o = {0.f, 0.f, 0.f, 0.f};
-        constexpr int kU = 4;   // parts asked for at once
-        for (int y = mine; y < pieces; y += kU * groups) {
-            float2 part[kU];
-            F4 x[kU];
+    for (int k = 0; k < kWaves; ++k) m = fmaxf(m, tops[k]);
+    F4 o = {0.f, 0.f, 0.f, 0.f};
+    add_parts(a, p, parts, r, d < a.D ? d : 0, tid / across, kThreads / across, pieces, m, &o, &l);
+    for (int k = across; k < kWave; k *= 2) {
+        l += __shfl_xor(l, k, kWave);
 #pragma unroll
-            for (int k = 0; k < kU; ++k) {
-                const int64_t z = row_of_part(min(y + k * groups, pieces - 1));
-                part[k] = p.ml[z];
-                x[k] = *(const F4*)(p.o + z * a.D + lane_d);
-            }
-#pragma unroll
-            for (int k = 0; k < kU; ++k) {
-                const float f = y + k * groups < pieces ? exp2_(part[k].x - m) : 0.f;
-                l += f * part[k].y;
-                o += f * x[k];
-            }
-        }
-        for (int k = across; k < kWave; k *= 2) {
-            l += __shfl_xor(l, k, kWave);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k, kWave);
-        }
-        if constexpr (kWide) {
-            sums[wave][threadIdx.x % kWave] = o;
-            weights[wave][threadIdx.x % kWave] = l;
-            __syncthreads();
-            if (wave == 0) {
-                o = F4{0.f, 0.f, 0.f, 0.f}, l = 0.f;
-#pragma unroll
-                for (int k = 0; k < kWaves; ++k) o += sums[k][lane], l += weights[k][lane];
-            }
-        }
-        if (lane < across && d < a.D) store4<T>((T*)a.out + row * a.D + d, o * (l > 0.f ? 1.f / l : 0.f));
-        if (lane == 0 && a.lse) a.lse[row] = lse_of(m, l);
-        if constexpr (kWide) __syncthreads();   // the sums' places are free for the next row
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], k, kWave);
     }
+    sums[wave][lane] = o;
+    weights[wave][lane] = l;
+    __syncthreads();
+    if (tid >= across) return;
+    o = F4{0.f, 0.f, 0.f, 0.f}, l = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) o += sums[k][lane], l += weights[k][lane];
+    if (d < a.D) store4<T>((T*)a.out + (int64_t)row * a.D + d, o * (l > 0.f ? 1.f / l : 0.f));
+    if (d == 0 && a.lse) a.lse[row] = lse_of(m, l);
 }
 
 // ---- launches ----
@@ -810,9 +851,9 @@ hipError_t attend_as(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
     if (e != hipSuccess || !p.split) return e;
     const int64_t rows = a.B * a.N * a.Hq;
     if (rows <= kWideRows)
-        k_attend_join<T, TR, KT, true><<<(unsigned)rows, kThreads, 0, s>>>(a, p);
+        k_attend_join_wide<T, TR, KT><<<(unsigned)rows, kThreads, 0, s>>>(a, p);
     else
-        k_attend_join<T, TR, KT, false><<<row_grid((rows + kWaves - 1) / kWaves, kThreads), kThreads, 0, s>>>(a, p);
+        k_attend_join<T, TR, KT><<<(unsigned)(a.B * a.Hk * p.tiles * (TR / kJoinRows)), kThreads, 0, s>>>(a, p);
     return hipGetLastError();
 }
 
