@@ -30,10 +30,14 @@ constexpr int kWideRows = 2048;       // most rows whose parts are joined by a w
 constexpr float kLow = -1e30f;        // below every score
 constexpr float kNone = -1e36f;       // where a running maximum begins: below kLow * scale, the floats far
 
-// Numerators are at most 2^kUp: float16's smallest normal number would otherwise be 2^-14 of the
-// largest, and a long context's many small ones would lose their digits or vanish.
+// A row's numerators are 2^(exponent - m + kUp), m its maximum so far: float16's smallest normal number
+// would otherwise be 2^-14 of the largest, and a long context's many small ones would lose their digits or
+// vanish.  m may lag behind by kLag before what was summed is brought up to it (8 rows of 64 by 64 heads
+// over 4500 slots: 121 us with no lag, 117 so); float16's largest numerators stay below 2^15.5.
 template <class T>
 constexpr float kUp = std::is_same_v<T, F16> ? 14.f : 0.f;
+template <class T>
+constexpr float kLag = std::is_same_v<T, F16> ? 1.f : 8.f;
 
 typedef float F4 __attribute__((ext_vector_type(4)));
 typedef uint32_t Quad __attribute__((ext_vector_type(4)));
@@ -126,7 +130,7 @@ struct Work {
 };
 
 struct WalkShared {
-    uint64_t before[kSplitBatch + 1];
+    uint64_t before[kSplitBatch];
     uint64_t sum[kWaves];
 };
 
@@ -434,7 +438,7 @@ struct RowsOf {
                 for (int e = 0; e < 4; ++e) most = fmaxf(most, s[x][t][e]);
             most = fmaxf(most, __shfl_xor(most, 16, kWave));
             most = fmaxf(most, __shfl_xor(most, 32, kWave)) * c2 - kUp<T>;
-            if (__any(most > m[x])) {
+            if (__any(most > m[x] + kLag<T>)) {
                 const float to = fmaxf(most, m[x]), f = exp2_(m[x] - to);
                 m[x] = to;
                 l[x] *= f;
@@ -597,17 +601,22 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
             if (lane < KT) sh.place[u % NS][lane] = place_of(a, w.head, sh.ids[u % NS][lane], at, j < w.end);
         };
         auto fetch = [&](int u) {
-            Place from[kPass];   // all of them first: LDS would be waited for before each load
+            // (some of the places first: LDS would be waited for before each load)
+            constexpr int kSome = M == 2 || DP == 256 ? kPass / 2 : kPass;
 #pragma unroll
-            for (int i = 0; i < kPass; ++i) from[i] = sh.place[u % NS][(i * kThreads + tid) / kRow];
+            for (int i0 = 0; i0 < kPass; i0 += kSome) {
+                Place from[kSome];
 #pragma unroll
-            for (int i = 0; i < kPass; ++i) {
-                const int x = i * kThreads + tid, slot = x / kRow, at = x % kRow;
-                const int to = (i * kThreads + wave * kWave) * 8;
-                const short* k = from[i].k + Tile<DP>::element(at ^ Tile<DP>::k_swap(slot), a.D);
-                const short* v = from[i].v + Tile<DP>::element(at ^ Tile<DP>::v_swap(slot), a.D);
-                load_to_lds(k, sh.k[u % NS] + to, p.tiles == 1);
-                load_to_lds(v, sh.v[u % NS] + to, p.tiles == 1);
+                for (int i = 0; i < kSome; ++i) from[i] = sh.place[u % NS][((i0 + i) * kThreads + tid) / kRow];
+#pragma unroll
+                for (int i = 0; i < kSome; ++i) {
+                    const int x = (i0 + i) * kThreads + tid, slot = x / kRow, at = x % kRow;
+                    const int to = ((i0 + i) * kThreads + wave * kWave) * 8;
+                    const short* k = from[i].k + Tile<DP>::element(at ^ Tile<DP>::k_swap(slot), a.D);
+                    const short* v = from[i].v + Tile<DP>::element(at ^ Tile<DP>::v_swap(slot), a.D);
+                    load_to_lds(k, sh.k[u % NS] + to, p.tiles == 1);
+                    load_to_lds(v, sh.v[u % NS] + to, p.tiles == 1);
+                }
             }
         };
         for (int x = tid; x < NS * KT; x += kThreads) {
@@ -644,7 +653,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
             if (first >= w.s.rows) continue;
             F4 s[M][KT / 16];
             S8 n[M][R::kPairs];
+            __builtin_amdgcn_s_setprio(1);   // (the other workgroup's wave then does its exponentials)
             rows.scores(sh.k[u % NS], q, s);
+            __builtin_amdgcn_s_setprio(0);
             if ((u + 1) * KT > w.start) {
 #pragma unroll
                 for (int x = 0; x < M; ++x) {
@@ -655,7 +666,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
                 }
             }
             rows.numerators(s, n, a.c2);
+            __builtin_amdgcn_s_setprio(1);
             rows.values(sh.v[u % NS], n);
+            __builtin_amdgcn_s_setprio(0);
         }
         rows.finish();
         const int own = afresh(lane);
