@@ -10,6 +10,8 @@
 // of a token that is nearly certain, and its log p, keep their digits: they are the others' sum.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "token.h"
 
 namespace tsc {
@@ -18,6 +20,10 @@ namespace {
 constexpr int kPartThreads = 256;
 constexpr int kWantParts = 1024;   // workgroups that fill the chip
 constexpr int kMinPart = 4096;     // tokens of a part
+// Vectors of a row that a thread holds in LDS between the two walks.  8192 rows of 131072 bfloat16 with
+// their gradient by 512 threads, us: 870 without, 850 with 2, 832 with 4, 815 with 6, 825 with 9 (two
+// workgroups a CU instead of three), 1026 with 10 (one); 859 by 1024 threads with 9.
+constexpr int kHold = 6;
 
 struct Row {
     float m, gain, slope;   // elsewhere
@@ -112,7 +118,8 @@ __device__ Spread sums_again(const T* x, int lo, int hi, int z, float c, float4*
 
 // kGrad: the row is read again, backwards: what was read last is nearest.  kEntropy: of the gradient.
 template <class T, int NT, bool kGrad, bool kEntropy>
-__global__ __launch_bounds__(NT) void k_score(ScoreArgs a) {
+__global__ __launch_bounds__(NT) void k_score(ScoreArgs a, int hold) {
+    extern __shared__ Vec4 held[];   // kGrad: a thread's first `hold` vectors
     __shared__ float4 red[NT / kWave];
     constexpr int W = kVec<T>, kU = kGrad ? 2 : 4;   // vectors asked for at once
     const int tid = threadIdx.x, V = a.V, nv = V / W;
@@ -146,6 +153,24 @@ __global__ __launch_bounds__(NT) void k_score(ScoreArgs a) {
             sums.push(v, c);
         };
         int i = tid;
+        const int kept = kGrad ? min(hold * NT, nv) : 0;   // vectors that are
+        if constexpr (kGrad) {
+            for (; i + (kU - 1) * NT < kept; i += kU * NT) {
+                Raw<T> r[kU];
+#pragma unroll
+                for (int u = 0; u < kU; ++u) r[u] = load_raw<T, true>(from(i + u * NT));
+#pragma unroll
+                for (int u = 0; u < kU; ++u) {
+                    held[i + u * NT] = {r[u].w[0], r[u].w[1], r[u].w[2], r[u].w[3]};
+                    push(r[u], i + u * NT);
+                }
+            }
+            for (; i < kept; i += NT) {
+                const Raw<T> r = load_raw<T, true>(from(i));
+                held[i] = {r.w[0], r.w[1], r.w[2], r.w[3]};
+                push(r, i);
+            }
+        }
         for (; i + (kU - 1) * NT < nv; i += kU * NT) {
             Raw<T> r[kU];
 #pragma unroll
@@ -167,7 +192,7 @@ __global__ __launch_bounds__(NT) void k_score(ScoreArgs a) {
         if constexpr (kGrad) {
             if (e < V) grad[e] = from_f<T>(e == z ? r.at_z : grad_of<kEntropy>(to_f(x[e]), r, c));
             i = tid + (nv > tid ? (nv - 1 - tid) / NT * NT : -NT);
-            for (; i - (kU - 1) * NT >= 0; i -= kU * NT) {
+            for (; i - (kU - 1) * NT >= kept; i -= kU * NT) {
                 Raw<T> q[kU];
 #pragma unroll
                 for (int u = 0; u < kU; ++u) q[u] = load_raw<T, true>(from(i - u * NT));
@@ -175,8 +200,12 @@ __global__ __launch_bounds__(NT) void k_score(ScoreArgs a) {
                 for (int u = 0; u < kU; ++u)
                     store_grad<T, kEntropy>(to(i - u * NT), q[u], r, (i - u * NT) * W, z, c);
             }
-            for (; i >= 0; i -= NT)
+            for (; i >= kept; i -= NT)
                 store_grad<T, kEntropy>(to(i), load_raw<T, true>(from(i)), r, i * W, z, c);
+            for (; i >= 0; i -= NT) {
+                const Vec4 q = held[i];
+                store_grad<T, kEntropy>(to(i), {{q.x, q.y, q.z, q.w}}, r, i * W, z, c);
+            }
         }
     }
 }
@@ -299,12 +328,17 @@ hipError_t launch_score(const ScoreArgs& a, hipStream_t s) {
         auto go = [&](auto nt) {
             constexpr int NT = decltype(nt)::value;
             const unsigned g = row_grid(rows, NT);
-            if (!a.grad)
-                k_score<T, NT, false, false><<<g, NT, 0, s>>>(a);
-            else if (a.entropy_weights)
-                k_score<T, NT, true, true><<<g, NT, 0, s>>>(a);
+            if (!a.grad) {
+                k_score<T, NT, false, false><<<g, NT, 0, s>>>(a, 0);
+                return;
+            }
+            const int64_t vectors = a.V / kVec<T>;
+            const int hold = (int)std::min<int64_t>((vectors + NT - 1) / NT, kHold);
+            const size_t lds = (size_t)hold * NT * sizeof(Vec4);
+            if (a.entropy_weights)
+                k_score<T, NT, true, true><<<g, NT, lds, s>>>(a, hold);
             else
-                k_score<T, NT, true, false><<<g, NT, 0, s>>>(a);
+                k_score<T, NT, true, false><<<g, NT, lds, s>>>(a, hold);
         };
         if (a.V <= 1024 || (a.V <= 8192 && rows >= 2048))
             go(std::integral_constant<int, 64>{});
