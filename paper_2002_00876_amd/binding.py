@@ -577,38 +577,43 @@ def verify(target, draft, tokens, uniforms, noise, lengths=None, draft_lse=None,
 _Strides = {n: ctypes.c_int64 * n for n in (3, 9)}
 
 
-def _prep_heads(x, name, dtype=None, shape=None, device=None):
+def _prep_heads(x, name):
     """x [B, N, H, D] with heads that start at multiples of 16 bytes (copied only where they do
     not) and contiguous elements, and its strides."""
     if not x.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if x.dim() != 4 or x.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError(f"{name} must be bfloat16 or float16 [B, N, H, D]")
-    if (dtype, shape, device) != (None, None, None) and (
-            x.dtype != dtype or tuple(x.shape) != shape or x.device != device):
-        raise ValueError(f"{name} must be {dtype} {list(shape)} on {device}")
     sb, sn, sh, sd = x.stride()
-    if sd != 1 or sb % 8 or sn % 8 or sh % 8 or x.data_ptr() % 16:
+    if sd != 1 or (sb | sn | sh) & 7 or x.data_ptr() & 15:
         # (a size of 1 may have any stride: a copy gives it an ordinary one)
         x = x.clone(memory_format=torch.contiguous_format)
         sb, sn, sh, sd = x.stride()
     return x, (sb, sn, sh)
 
 
-def _prep_cache(k_cache, v_cache, pages, starts, lengths, B, dtype, device):
-    for x, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if x.dim() != 4 or x.dtype != dtype or x.device != device:
-            raise ValueError(f"{name} must be {dtype} [P, S, Hk, D] on {device}")
-    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
-        raise ValueError("k_cache and v_cache must have the same shape and strides")
-    if k_cache.shape[3] > 1 and k_cache.stride(3) != 1:
+def _same(x, name, shape, like):
+    if x.dtype != like.dtype or x.shape != shape or x.device != like.device:
+        raise ValueError(f"{name} must be {like.dtype} {list(shape)} on {like.device}")
+
+
+def _prep_cache(k_cache, v_cache, pages, starts, lengths, like):
+    """The caches' layout, and the whole numbers, of tensors that belong to `like` [B, N, H, D]."""
+    shape, stride, device = k_cache.shape, k_cache.stride(), like.device
+    if len(shape) != 4 or k_cache.dtype != like.dtype or k_cache.device != device:
+        raise ValueError(f"k_cache must be {like.dtype} [P, S, Hk, D] on {device}")
+    _same(v_cache, "v_cache", shape, like)
+    if v_cache.stride() != stride:
+        raise ValueError("k_cache and v_cache must have the same strides")
+    if shape[3] > 1 and stride[3] != 1:
         raise ValueError("the elements of a head of the caches must be contiguous")
     if pages.dim() != 2:
         raise ValueError("pages must be int32 [B, M]")
+    B = like.shape[0]
     pages = _prep_small(pages, "pages", torch.int32, (B, pages.shape[1]), device)
     starts = _prep_small(starts, "starts", torch.int32, (B,), device)
     lengths = _prep_small(lengths, "lengths", torch.int32, (B,), device)
-    return CacheLayout(*k_cache.shape, *k_cache.stride()[:3]), pages, starts, lengths
+    return CacheLayout(*shape, *stride[:3]), pages, starts, lengths
 
 
 def cache_append(k, v, k_cache, v_cache, pages, starts, lengths=None, q=None, freqs=None,
@@ -624,9 +629,9 @@ def cache_append(k, v, k_cache, v_cache, pages, starts, lengths=None, q=None, fr
     k, ks = _prep_heads(k, "k")
     B, N, Hk, D = k.shape
     dtype, dev = k.dtype, k.device
-    v, vs = _prep_heads(v, "v", dtype, (B, N, Hk, D), dev)
-    layout, pages, starts, lengths = _prep_cache(k_cache, v_cache, pages, starts, lengths, B, dtype,
-                                                 dev)
+    v, vs = _prep_heads(v, "v")
+    _same(v, "v", k.shape, k)
+    layout, pages, starts, lengths = _prep_cache(k_cache, v_cache, pages, starts, lengths, k)
     if k_cache.shape[2:] != (Hk, D):
         raise ValueError(f"the caches must be [P, S, {Hk}, {D}]")
     positions = _prep_small(positions, "positions", torch.int32, (B, N), dev)
@@ -636,8 +641,9 @@ def cache_append(k, v, k_cache, v_cache, pages, starts, lengths=None, q=None, fr
         freqs = _prep_small(freqs, "freqs", torch.float32, (R // 2,), dev)
     Hq, qs = 0, (0, 0, 0)
     if q is not None:
-        Hq = q.shape[2] if q.dim() == 4 else 0
-        q, qs = _prep_heads(q, "q", dtype, (B, N, Hq, D), dev)
+        q, qs = _prep_heads(q, "q")
+        Hq = q.shape[2]
+        _same(q, "q", (B, N, Hq, D), k)
         if out is None:
             out = torch.empty((B, N, Hq, D), dtype=dtype, device=dev)
         else:
@@ -667,8 +673,7 @@ def tree_attention(q, k_cache, v_cache, pages, starts, parents=None, lengths=Non
     q, qs = _prep_heads(q, "q")
     B, N, Hq, D = q.shape
     dtype, dev = q.dtype, q.device
-    layout, pages, starts, lengths = _prep_cache(k_cache, v_cache, pages, starts, lengths, B, dtype,
-                                                 dev)
+    layout, pages, starts, lengths = _prep_cache(k_cache, v_cache, pages, starts, lengths, q)
     if k_cache.shape[3] != D:
         raise ValueError(f"the caches must be [P, S, Hk, {D}]")
     parents = _prep_small(parents, "parents", torch.int32, (B, N), dev)

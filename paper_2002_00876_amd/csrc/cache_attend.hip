@@ -99,17 +99,16 @@ struct Shape {
     int rows, units, tiles;   // of a sequence: rows, units of a row tile, row tiles of a key head
 };
 
-__device__ __forceinline__ int slots_seen(const AttendArgs& a, int64_t b, int n) {
-    return min(slots_before(a.c, b) + n, a.c.M * a.c.S);
+__device__ __forceinline__ int2 size_of(const AttendArgs& a, int64_t b) {   // drafts, slots before them
+    return make_int2(new_tokens(a.c, b, a.N), slots_before(a.c, b));
 }
 
 template <int TR, int KU>
-__device__ __forceinline__ Shape shape_of(const AttendArgs& a, int64_t b) {
-    const int n = new_tokens(a.c, b, a.N), G = a.Hq / a.Hk;
+__device__ __forceinline__ Shape shape_of(const AttendArgs& a, int2 size) {
     Shape s;
-    s.rows = n * G;
+    s.rows = size.x * (a.Hq / a.Hk);
     s.tiles = (s.rows + TR - 1) / TR;
-    s.units = n ? (slots_seen(a, b, n) + KU - 1) / KU : 0;
+    s.units = size.x ? (min(size.y + size.x, a.c.M * a.c.S) + KU - 1) / KU : 0;
     return s;
 }
 
@@ -120,17 +119,19 @@ struct Work {
     int n, start, end;              // drafts, slots before them, all slots
     int head, tile, lo, hi, part;   // part < 0: all of its units
 
-    __device__ __forceinline__ void of(const AttendArgs& a, int b_, Shape s_) {
+    template <int TR, int KU>
+    __device__ __forceinline__ void of(const AttendArgs& a, int b_, int2 size) {
         b = b_;
-        s = {uniform(s_.rows), uniform(s_.units), uniform(s_.tiles)};
-        n = s.rows / (a.Hq / a.Hk);
-        start = uniform(slots_before(a.c, b));
+        n = uniform(size.x);
+        start = uniform(size.y);
+        s = shape_of<TR, KU>(a, make_int2(n, start));
         end = min(start + n, a.c.M * a.c.S);
     }
 };
 
 struct WalkShared {
     uint64_t before[kSplitBatch];
+    int2 size[kSplitBatch];   // drafts, slots before them
     uint64_t sum[kWaves];
 };
 
@@ -161,8 +162,10 @@ struct Walk {
             const int b = tid * kEach + k;
             mine[k] = 0;
             if (b < a.B) {
-                const Shape s = shape_of<TR, KU>(a, b);
+                const int2 size = size_of(a, b);
+                const Shape s = shape_of<TR, KU>(a, size);
                 mine[k] = (uint64_t)s.units * s.tiles;
+                sh.size[b] = size;
             }
             all += mine[k];
         }
@@ -205,7 +208,7 @@ struct Walk {
         if (at >= end) return false;
         if (!p.split) {
             const int each = a.Hk * p.tiles, b = stretch / each, rest = stretch - b * each;
-            w->of(a, b, shape_of<TR, KU>(a, b));
+            w->template of<TR, KU>(a, b, size_of(a, b));
             w->head = rest / p.tiles;
             w->tile = rest % p.tiles;
             w->lo = 0;
@@ -222,7 +225,7 @@ struct Walk {
             else
                 more = mid;
         }
-        w->of(a, b, shape_of<TR, KU>(a, b));
+        w->template of<TR, KU>(a, b, sh.size[b]);
         const uint64_t in = at - uniform(sh.before[b]);
         const int tile = uniform((int)(in >> 32 ? in / (uint32_t)w->s.units : (uint32_t)in / (uint32_t)w->s.units));
         w->lo = (int)(in - (uint64_t)tile * w->s.units);
@@ -238,16 +241,12 @@ struct Walk {
 // ---- who sees whom ----
 
 // Bit j of node i's words: draft i follows draft j, or is j.  Steps of 1, 2, 4, ... drafts towards the
-// text: after as many as N has bits every one is known.  Every thread calls it.
-__device__ void find_ancestors(const AttendArgs& a, int64_t b, int n, uint32_t* words, short* up) {
+// text: after as many as N has bits every one is known.  Every thread calls it, with draft threadIdx.x's
+// parent as it was given.
+__device__ void find_ancestors(const AttendArgs& a, int n, int parent, uint32_t* words, short* up) {
     const int i = threadIdx.x, W = (a.N + 31) / 32;   // kThreads >= kMaxNodes
     uint32_t mine[kWords];
-    int parent = -1;
-    if (i < n) {
-        parent = a.parents[b * a.N + i];
-        if (parent >= i) parent = -1;
-        if (parent < 0) parent = -1;
-    }
+    if (parent >= i || parent < 0) parent = -1;
 #pragma unroll
     for (int w = 0; w < kWords; ++w) mine[w] = i / 32 == w ? 1u << (i % 32) : 0u;
     for (int reach = 1; reach < n; reach *= 2) {
@@ -619,18 +618,21 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
                 }
             }
         };
+        // what has to be waited for is asked for at once: parents, queries, page numbers
+        const bool forks = a.parents && hi * KT > w.start;
+        const int parent = forks && tid < w.n ? a.parents[w.b * a.N + tid] : -1;
+        S8 q[M][DP / 32];
+#pragma unroll
+        for (int x = 0; x < M; ++x)
+#pragma unroll
+            for (int y = 0; y < DP / 32; ++y) q[x][y] = query(a, w, first + x * 16 + lane % 16, y);
         for (int x = tid; x < NS * KT; x += kThreads) {
             const int u = lo + x / KT, j = u * KT + x % KT;
             int at;
             const int page = page_of(a.c, min(j, w.end - 1), &at);
             sh.place[u % NS][x % KT] = place_of(a, w.head, pages[page], at, j < w.end);
         }
-        S8 q[M][DP / 32];
-#pragma unroll
-        for (int x = 0; x < M; ++x)
-#pragma unroll
-            for (int y = 0; y < DP / 32; ++y) q[x][y] = query(a, w, first + x * 16 + lane % 16, y);
-        if (a.parents && hi * KT > w.start) find_ancestors(a, w.b, w.n, sh.words, sh.up);
+        if (forks) find_ancestors(a, w.n, parent, sh.words, sh.up);
         loads_done<0>();   // (what has results)
         __syncthreads();
         if (wave == 0)
@@ -699,7 +701,7 @@ struct Parts {
 
     __device__ __forceinline__ Parts(const AttendArgs& a, const AttendPlan& p, int64_t b, int head, int tile) {
         const int per = *p.per;
-        const Shape s = shape_of<TR, KU>(a, b);
+        const Shape s = shape_of<TR, KU>(a, size_of(a, b));
         pieces = first = begun = 0;
         step = 2 * a.Hk;
         rows = s.rows - tile * TR;
@@ -823,7 +825,7 @@ AttendPlan attend_plan(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D, 
     AttendPlan p{};
     p.tiles = (int)((N * (Hq / Hk) + TR - 1) / TR);
     p.split = B <= kSplitBatch;
-    p.least = 2;
+    p.least = 1;
     const int64_t items = B * Hk * p.tiles;
     // (a multiple of 8 of them, as each XCD takes an eighth)
     p.grid = (unsigned)(p.split ? (std::max(kWant / Hk, (int64_t)1) * Hk + 7) / 8 * 8 : (items + 7) / 8 * 8);
