@@ -61,7 +61,8 @@ typedef struct ts_cache_layout {
  *   positions  int32 [B, N] or NULL: the position of each new token (a draft's depth in its tree counts,
  *            not its slot); NULL: its slot.
  *   q_out    [B, N, Hq, D], contiguous (may be q itself where q is); zeros for padding.
- * No page may be written through two places: what lies in such slots is that of one of them.
+ * k, v and q do not overlap the caches, and no slot is written twice in a call (it would hold what one of
+ * the two writes).
  */
 ts_status ts_cache_append(const void* k, const void* v, const void* q, const int64_t strides[9],
                           int dtype, const float* freqs, int64_t R, int neighbours,
@@ -79,14 +80,14 @@ size_t ts_cache_attend_workspace_bytes(int64_t B, int64_t N, int64_t Hq, int64_t
  *   parents  int32 [B, N] or NULL: the draft that draft i continues, below i; -1 (or anything outside
  *            [0, i)): it continues the text before the drafts.  NULL: a path, parents[i] = i - 1.
  *   N        at most ts_cache_max_nodes().
- *   scale    > 0, at most 1e6: out_i = sum_j p_j v_j, p = softmax(scale * q_i . k_j) over the slots j
+ *   scale    in [1e-6, 1e6]: out_i = sum_j p_j v_j, p = softmax(scale * q_i . k_j) over the slots j
  *            before starts[b], the drafts that i follows, and i itself.
  *   out      [B, N, Hq, D], contiguous; lse float32 [B, N, Hq] or NULL: log sum_j exp(scale q_i . k_j).
  *            Where no slot is seen out is 0 and lse -inf, and so they are for padding.
  *   ws       device workspace of at least ts_cache_attend_workspace_bytes(...), aligned to 256
  *            bytes.  Its contents on entry are ignored.
- * Keys and values of slots before starts[b] + lengths[b] are finite, and so are queries; what lies
- * behind them is never used.
+ * Queries, keys and values of slots before starts[b] + lengths[b] are finite, and products q . k within
+ * 1e30 in size; what lies behind these slots is never used.
  */
 ts_status ts_cache_attend(const void* q, const int64_t strides[3], int dtype, const void* k_cache,
                           const void* v_cache, const ts_cache_layout* layout,

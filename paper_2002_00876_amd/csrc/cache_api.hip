@@ -188,8 +188,8 @@ ts_status ts_cache_attend(const void* q, const int64_t strides[3], int dtype, co
             return bad(call, TS_ERR_BAD_DIM, "N must be at most " + std::to_string(kMaxNodes) +
                                                  ", and the call's row tiles some 2^23");
         if ((st = check_half(call, dtype)) || (st = check_aligned(call, "q", q, strides))) return st;
-        if (!(scale > 0.f && scale <= 1e6f))
-            return bad(call, TS_ERR_BAD_ARG, "scale must be in (0, 1e6]");
+        if (!(scale >= 1e-6f && scale <= 1e6f))
+            return bad(call, TS_ERR_BAD_ARG, "scale must be in [1e-6, 1e6]");
         if (reinterpret_cast<uintptr_t>(out) % 16)
             return bad(call, TS_ERR_BAD_ARG, "out must start at a multiple of 16 bytes");
         if ((st = check_ws(call, attend_workspace(B, N, Hq, Hk, D), ws, ws_bytes))) return st;

@@ -94,7 +94,7 @@ def test_bad_types_strides_and_alignment_are_rejected(L):
             assert f(L, s=strides(9, value)) == BAD_ARG
     for bad in (dict(k=FAKE + 8), dict(v=FAKE + 8)):
         assert append(L, **bad) == BAD_ARG
-    for scale in (0.0, -1.0, math.nan, math.inf, 1e7):
+    for scale in (0.0, -1.0, math.nan, math.inf, 1e7, 1e-7):
         assert attend(L, scale=scale) == BAD_ARG
     for f in (score, score_grad):
         for bad in (dict(dt=3), dict(sb=-1), dict(sn=1 << 41), dict(T=0.0), dict(T=math.nan)):

@@ -130,7 +130,7 @@ def test_many_small_numerators():
             _compare(d, _run(d))
 
 
-@pytest.mark.parametrize("B", [1, 5, 64, 512, 513, 700])
+@pytest.mark.parametrize("B", [1, 5, 63, 64, 65, 129, 255, 256, 257, 700])
 @pytest.mark.parametrize("N,tree", [(1, False), (6, True)])
 def test_batches(B, N, tree):
     _check(B, N, 2, 1, 64, 16, 150, tree=tree, seed=B)
@@ -144,6 +144,23 @@ def test_one_long_sequence_among_short_ones():
     d["pages"] = rng.permutation(P)[:40 * M].reshape(40, M)
     d["k"], d["v"] = d["k"].nan_to_num(0.3), d["v"].nan_to_num(0.3)
     _compare(d, _run(d))
+
+
+@pytest.mark.parametrize("D", [64, 128, 200])
+@pytest.mark.parametrize("N,G", [(3, 2), (40, 2), (60, 5)])
+def test_stretches_of_several_sequences(D, N, G):
+    # more units than workgroups: stretches that end within one sequence and begin within another
+    _check(90, N, G, 1, D, 16, 900, seed=D + N, wide=0)
+
+
+@pytest.mark.parametrize("Hk", [3, 7, 12, 40])
+def test_heads_that_do_not_divide_the_workgroups(Hk):
+    for N in (2, 70):
+        _check(5, N, Hk, Hk, 64, 16, 700, seed=Hk)
+
+
+def test_more_heads_than_workgroups():
+    _check(2, 2, 600, 600, 8, 16, 300, seed=1)
 
 
 def test_empty_rows():
