@@ -79,10 +79,11 @@ size_t ts_cache_attend_workspace_bytes(int64_t B, int64_t N, int64_t Hq, int64_t
  *   q        [B, N, Hq, D], elements from a sequence, a token, a head to the next in strides[0..2].
  *   parents  int32 [B, N] or NULL: the draft that draft i continues, below i; -1 (or anything outside
  *            [0, i)): it continues the text before the drafts.  NULL: a path, parents[i] = i - 1.
- *   N        at most ts_cache_max_nodes().
+ *   N        at most ts_cache_max_nodes().  With up to 256 sequences B * ceil(N * Hq / (64 * Hk)) * M * S up to
+ *            2^35 always fits; what the kernels' numbers do not hold is refused (TS_ERR_BAD_DIM).
  *   scale    in [1e-6, 1e6]: out_i = sum_j p_j v_j, p = softmax(scale * q_i . k_j) over the slots j
  *            before starts[b], the drafts that i follows, and i itself.
- *   out      [B, N, Hq, D], contiguous; lse float32 [B, N, Hq] or NULL: log sum_j exp(scale q_i . k_j).
+ *   out      [B, N, Hq, D], contiguous, not overlapping q; lse float32 [B, N, Hq] or NULL: log sum_j exp(scale q_i . k_j).
  *            Where no slot is seen out is 0 and lse -inf, and so they are for padding.
  *   ws       device workspace of at least ts_cache_attend_workspace_bytes(...), aligned to 256
  *            bytes.  Its contents on entry are ignored.

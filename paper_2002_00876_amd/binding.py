@@ -364,7 +364,7 @@ def _prep_small(x, name, dtype, shape, device):
     if x is None:
         return None
     if x.dtype != dtype or x.shape != shape or x.device != device:
-        raise ValueError(f"{name} must be {dtype} {list(shape)} on the same device as the logits")
+        raise ValueError(f"{name} must be {dtype} {list(shape)} on {device}")
     return x if x.is_contiguous() else x.contiguous()
 
 
@@ -373,8 +373,7 @@ def _check_outs(out, names, dtypes, shapes, device):
         raise ValueError(f"out must be ({', '.join(names)})")
     for x, name, dtype, shape in zip(out, names, dtypes, shapes):
         if x.dtype != dtype or x.shape != shape or x.device != device or not x.is_contiguous():
-            raise ValueError(f"{name} must be contiguous {dtype} {list(shape)} on the same device "
-                             "as the logits")
+            raise ValueError(f"{name} must be contiguous {dtype} {list(shape)} on {device}")
     return out
 
 

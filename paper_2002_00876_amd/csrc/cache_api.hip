@@ -15,7 +15,6 @@ namespace {
 
 constexpr int64_t kMaxQueryHeads = 1024;
 constexpr int64_t kMaxSlots = (int64_t)1 << 30;
-constexpr int64_t kMaxGrid = (int64_t)1 << 23;   // workgroups of 256 threads, with room to 2^32
 
 bool heads_ok(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D) {
     return B >= 1 && N >= 1 && Hq >= 1 && Hk >= 1 && Hq <= kMaxQueryHeads && Hq % Hk == 0 &&
@@ -184,9 +183,10 @@ ts_status ts_cache_attend(const void* q, const int64_t strides[3], int dtype, co
             return st;
         const int64_t Hk = layout->heads, D = layout->head_size;
         if ((st = check_heads(call, B, N, Hq, Hk, D))) return st;
-        if (N > kMaxNodes || attend_grid(B, N, Hq, Hk, D) > kMaxGrid)
+        if (N > kMaxNodes || !attend_fits(B, N, Hq, Hk, D, M * layout->page_size))
             return bad(call, TS_ERR_BAD_DIM, "N must be at most " + std::to_string(kMaxNodes) +
-                                                 ", and the call's row tiles some 2^23");
+                                                 ", row tiles of all key heads 2^23, and a head's tiles of "
+                                                 "32 slots of them all 2^30 a workgroup");
         if ((st = check_half(call, dtype)) || (st = check_aligned(call, "q", q, strides))) return st;
         if (!(scale >= 1e-6f && scale <= 1e6f))
             return bad(call, TS_ERR_BAD_ARG, "scale must be in [1e-6, 1e6]");

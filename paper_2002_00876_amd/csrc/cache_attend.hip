@@ -13,6 +13,10 @@
 //
 // Numerators are rounded to the cache's type for the product (their sum is not): each is off by half a
 // step at most, as the values are themselves, and the products are summed in 32 bits.
+//
+// Few rows are bound by the read: 64 contexts of up to 8000 slots, 8 heads of 128, with up to 5 drafts of 32
+// heads 162 us, 5.9 TB/s.  Many are bound by the products and the exponentials beside them, which two waves a
+// SIMD do not hide of each other: 8 trees of 64 drafts of 64 heads over 4500 slots 117 us, 620 TFLOP/s.
 #include <algorithm>
 
 #include "cache.h"
@@ -66,8 +70,9 @@ __device__ __forceinline__ S4 read_turned(const short* at) {
 // A unit is a row tile's walk over KU slots of a key head.  A head's units of all row tiles, one tile after
 // the other, make a line that is cut into equal stretches, one a workgroup, whatever the lengths: none of
 // them waits for a longer one.  All heads' lines are cut alike and their stretches lie side by side, so that
-// the heads of a slot, which lie one behind the other in most caches, are read at about the same time (64
-// contexts of up to 8000 slots, 8 heads of 128: 184 us where each head had stretches of its own, and 169 so).
+// the heads of a slot, which lie one behind the other in most caches, are read at about the same time (a
+// context of 131072 slots, 4 heads of 64: 31 us where each head had stretches of its own, 28 so; no difference
+// to 64 contexts of up to 8000 slots with 8 heads of 128).
 // What a workgroup has of a row tile is written as a part where the tile goes on elsewhere; a stretch has two
 // such ends at most.
 struct AttendPlan {
@@ -891,9 +896,10 @@ hipError_t attend_type(const AttendArgs& a, const AttendPlan& p, hipStream_t s) 
 size_t attend_workspace(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D) {
     return attend_plan(B, N, Hq, Hk, D, nullptr).bytes;
 }
-int64_t attend_grid(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D) {
-    const int64_t TR = 16 * kWaves * sixteens(N, Hq, Hk, D);
-    return B * Hk * ((N * (Hq / Hk) + TR - 1) / TR) + kWant + 8;
+bool attend_fits(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D, int64_t slots) {
+    const AttendPlan p = attend_plan(B, N, Hq, Hk, D, nullptr);
+    if (B * Hk * p.tiles > (int64_t)1 << 23) return false;   // 2^31 threads
+    return !p.split || B * p.tiles * (slots / 32 + 1) / (p.grid / Hk) < (int64_t)1 << 30;
 }
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
     const AttendPlan p = attend_plan(a.B, a.N, a.Hq, a.Hk, a.D, a.ws);

@@ -54,8 +54,9 @@ struct AttendArgs {
     void* ws;
 };
 size_t attend_workspace(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D);
-// Workgroups that the call launches at most
-int64_t attend_grid(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D);
+// Whether the call's workgroups, and a workgroup's units where sequences have `slots` slots at most, are
+// numbers that its kernels hold
+bool attend_fits(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D, int64_t slots);
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s);
 
 }  // namespace tsc

@@ -119,7 +119,7 @@ __device__ Spread sums_again(const T* x, int lo, int hi, int z, float c, float4*
 // kGrad: the row is read again, backwards: what was read last is nearest.  kEntropy: of the gradient.
 template <class T, int NT, bool kGrad, bool kEntropy>
 __global__ __launch_bounds__(NT) void k_score(ScoreArgs a, int hold) {
-    extern __shared__ Vec4 held[];   // kGrad: a thread's first `hold` vectors
+    extern __shared__ uint4 held[];   // kGrad: a thread's first `hold` vectors
     __shared__ float4 red[NT / kWave];
     constexpr int W = kVec<T>, kU = kGrad ? 2 : 4;   // vectors asked for at once
     const int tid = threadIdx.x, V = a.V, nv = V / W;
@@ -161,13 +161,13 @@ __global__ __launch_bounds__(NT) void k_score(ScoreArgs a, int hold) {
                 for (int u = 0; u < kU; ++u) r[u] = load_raw<T, true>(from(i + u * NT));
 #pragma unroll
                 for (int u = 0; u < kU; ++u) {
-                    held[i + u * NT] = {r[u].w[0], r[u].w[1], r[u].w[2], r[u].w[3]};
+                    held[i + u * NT] = make_uint4(r[u].w[0], r[u].w[1], r[u].w[2], r[u].w[3]);
                     push(r[u], i + u * NT);
                 }
             }
             for (; i < kept; i += NT) {
                 const Raw<T> r = load_raw<T, true>(from(i));
-                held[i] = {r.w[0], r.w[1], r.w[2], r.w[3]};
+                held[i] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
                 push(r, i);
             }
         }
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(NT) void k_score(ScoreArgs a, int hold) {
             for (; i >= kept; i -= NT)
                 store_grad<T, kEntropy>(to(i), load_raw<T, true>(from(i)), r, i * W, z, c);
             for (; i >= 0; i -= NT) {
-                const Vec4 q = held[i];
+                const uint4 q = held[i];
                 store_grad<T, kEntropy>(to(i), {{q.x, q.y, q.z, q.w}}, r, i * W, z, c);
             }
         }
@@ -334,7 +334,7 @@ hipError_t launch_score(const ScoreArgs& a, hipStream_t s) {
             }
             const int64_t vectors = a.V / kVec<T>;
             const int hold = (int)std::min<int64_t>((vectors + NT - 1) / NT, kHold);
-            const size_t lds = (size_t)hold * NT * sizeof(Vec4);
+            const size_t lds = (size_t)hold * NT * sizeof(uint4);
             if (a.entropy_weights)
                 k_score<T, NT, true, true><<<g, NT, lds, s>>>(a, hold);
             else

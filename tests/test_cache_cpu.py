@@ -76,6 +76,8 @@ def test_bad_dimensions_are_rejected(L):
         assert append(L, **bad) == BAD_DIM, bad
     assert attend(L, N=257) == BAD_DIM
     assert attend(L, B=1 << 23, Hk=2, Hq=2, N=1) == BAD_DIM
+    assert attend(L, B=256, Hk=600, Hq=600, N=1, S=1 << 15, M=1 << 15) == BAD_DIM   # 2^33 units a stretch
+    assert attend(L, B=256, Hk=1, Hq=1, N=1, S=1 << 15, M=1 << 15, nb=0) == WORKSPACE
     assert "ts_cache_attend" in L.ts_last_error().decode()
     most_v = L.ts_token_max_vocab()
     for f in (score, score_grad):
