@@ -563,10 +563,11 @@ constexpr int kStages = DP == 64 ? 4 : 2;
 
 template <int DP, int KT, int NS>
 struct AttendShared {
+    static constexpr int kGroup = kThreads / KT;   // units whose places are looked up together
     short k[NS][KT * DP];
     short v[NS][KT * DP];
-    Place place[NS][KT];
-    int32_t ids[NS][KT];
+    Place place[kGroup + 1][KT];
+    int32_t ids[kThreads];
     WalkShared walk;
     short up[kMaxNodes];
     uint32_t words[];   // [N][ceil(N / 32)], where there are parents
@@ -579,6 +580,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
     constexpr int TR = 16 * M * kWaves, kRow = DP / 8, kPass = KT * kRow / kThreads;
     using Shared = AttendShared<DP, KT, NS>;
     using R = RowsOf<T, DP, M, KT>;
+    constexpr int kGroup = Shared::kGroup, kRing = kGroup + 1;
+    static_assert(kFar < kGroup, "the first group has what is fetched before the loop, and its first step's");
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Shared& sh = *(Shared*)lds;
     const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave);
@@ -591,18 +594,20 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
         }
         const int lo = w.lo, hi = w.hi, first = w.tile * TR + wave * 16 * M, G = a.Hq / a.Hk;
         const int32_t* pages = a.c.pages + w.b * a.c.M;
-        // Page numbers go to LDS, too, by the first wave, kFar units before they are made places of: the
-        // compiler would wait for all loads before it if one of them had a result.
-        auto ask = [&](int u) {
+        // The places of kGroup units from x on, a thread a slot.  Page numbers go to LDS, too, a group ahead:
+        // the compiler would wait for all loads before them if they had a result.
+        auto page_at = [&](int x, int* at) { return page_of(a.c, min(x * KT + tid, w.end - 1), at); };
+        auto ask = [&](int x) {
             int at;
-            const int page = page_of(a.c, min(u * KT + lane, w.end - 1), &at);
-            if (lane < KT) load_id_to_lds(pages + page, sh.ids[u % NS]);
+            load_id_to_lds(pages + page_at(x, &at), sh.ids + wave * kWave);
         };
-        auto find = [&](int u) {
-            const int j = u * KT + lane;
+        auto keep = [&](int x, int id, int at) {
+            sh.place[(x + tid / KT - lo) % kRing][tid % KT] = place_of(a, w.head, id, at, x * KT + tid < w.end);
+        };
+        auto find = [&](int x) {
             int at;
-            page_of(a.c, min(j, w.end - 1), &at);
-            if (lane < KT) sh.place[u % NS][lane] = place_of(a, w.head, sh.ids[u % NS][lane], at, j < w.end);
+            page_at(x, &at);
+            keep(x, sh.ids[tid], at);
         };
         auto fetch = [&](int u) {
             // (some of the places first: LDS would be waited for before each load)
@@ -611,7 +616,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
             for (int i0 = 0; i0 < kPass; i0 += kSome) {
                 Place from[kSome];
 #pragma unroll
-                for (int i = 0; i < kSome; ++i) from[i] = sh.place[u % NS][((i0 + i) * kThreads + tid) / kRow];
+                for (int i = 0; i < kSome; ++i) from[i] = sh.place[(u - lo) % kRing][((i0 + i) * kThreads + tid) / kRow];
 #pragma unroll
                 for (int i = 0; i < kSome; ++i) {
                     const int x = (i0 + i) * kThreads + tid, slot = x / kRow, at = x % kRow;
@@ -631,17 +636,13 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
         for (int x = 0; x < M; ++x)
 #pragma unroll
             for (int y = 0; y < DP / 32; ++y) q[x][y] = query(a, w, first + x * 16 + lane % 16, y);
-        for (int x = tid; x < NS * KT; x += kThreads) {
-            const int u = lo + x / KT, j = u * KT + x % KT;
-            int at;
-            const int page = page_of(a.c, min(j, w.end - 1), &at);
-            sh.place[u % NS][x % KT] = place_of(a, w.head, pages[page], at, j < w.end);
-        }
+        int token;
+        const int page = page_at(lo, &token);
+        keep(lo, pages[page], token);
         if (forks) find_ancestors(a, w.n, parent, sh.words, sh.up);
         loads_done<0>();   // (what has results)
         __syncthreads();
-        if (wave == 0)
-            for (int u = lo + NS; u < lo + NS + kFar; ++u) ask(u);
+        ask(lo + kGroup);
         for (int u = lo; u < min(lo + kFar, hi); ++u) fetch(u);
         R rows;
         rows.init();
@@ -653,9 +654,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
                 loads_done<0>();
             __syncthreads();
             if (u + kFar < hi) fetch(u + kFar);
-            if (wave == 0) {
-                ask(u + NS + kFar);
-                find(u + NS);
+            if ((u + kFar - lo) % kGroup == kGroup - 1 && u + kFar + 1 < hi) {
+                find(u + kFar + 1);
+                ask(u + kFar + 1 + kGroup);   // (its numbers are written where these have been read)
             }
             if (first >= w.s.rows) continue;
             F4 s[M][KT / 16];
