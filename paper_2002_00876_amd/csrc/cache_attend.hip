@@ -77,6 +77,7 @@ __device__ __forceinline__ S4 read_turned(const short* at) {
 // such ends at most.
 struct AttendPlan {
     int tiles;          // row tiles of a key head, of N drafts
+    int chunks;         // of kJoinRows rows of a tile that have rows
     int least;          // units of a stretch, at least
     bool split;         // otherwise a workgroup takes one row tile
     unsigned grid;
@@ -758,8 +759,8 @@ template <class T, int TR, int KU>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, AttendPlan p) {
     const int G = a.Hq / a.Hk, across = lanes_across(a.D), d = (int)threadIdx.x % across * 4;
     uint32_t at = blockIdx.x;
-    const int chunk = (int)(at % (TR / kJoinRows));
-    at /= TR / kJoinRows;
+    const int chunk = (int)(at % (uint32_t)p.chunks);
+    at /= (uint32_t)p.chunks;
     const int tile = (int)(at % (uint32_t)p.tiles);
     at /= (uint32_t)p.tiles;
     const int head = (int)(at % (uint32_t)a.Hk);
@@ -830,6 +831,7 @@ AttendPlan attend_plan(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D, 
     const int64_t TR = 16 * kWaves * sixteens(N, Hq, Hk, D);
     AttendPlan p{};
     p.tiles = (int)((N * (Hq / Hk) + TR - 1) / TR);
+    p.chunks = (int)((std::min(N * (Hq / Hk), TR) + kJoinRows - 1) / kJoinRows);
     p.split = B <= kSplitBatch;
     p.least = 1;
     const int64_t items = B * Hk * p.tiles;
@@ -874,7 +876,7 @@ hipError_t attend_as(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
     if (rows <= kWideRows)
         k_attend_join_wide<T, TR, KT><<<(unsigned)rows, kThreads, 0, s>>>(a, p);
     else
-        k_attend_join<T, TR, KT><<<(unsigned)(a.B * a.Hk * p.tiles * (TR / kJoinRows)), kThreads, 0, s>>>(a, p);
+        k_attend_join<T, TR, KT><<<(unsigned)(a.B * a.Hk * p.tiles * p.chunks), kThreads, 0, s>>>(a, p);
     return hipGetLastError();
 }
 
