@@ -16,7 +16,7 @@
 //
 // Few rows are bound by the read: 64 contexts of up to 8000 slots, 8 heads of 128, with up to 5 drafts of 32
 // heads 162 us, 5.9 TB/s.  Many are bound by the products and the exponentials beside them, which two waves a
-// SIMD do not hide of each other: 8 trees of 64 drafts of 64 heads over 4500 slots 117 us, 620 TFLOP/s.
+// SIMD do not hide of each other: 8 trees of 64 drafts of 64 heads over 4500 slots 113 us, 645 TFLOP/s.
 #include <algorithm>
 
 #include "cache.h"
@@ -612,7 +612,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
         };
         auto fetch = [&](int u) {
             // (some of the places first: LDS would be waited for before each load)
-            constexpr int kSome = M == 2 || DP == 256 ? kPass / 2 : kPass;
+            constexpr int kSome = DP == 256 ? 1 : M == 2 ? kPass / 2 : kPass;
 #pragma unroll
             for (int i0 = 0; i0 < kPass; i0 += kSome) {
                 Place from[kSome];

