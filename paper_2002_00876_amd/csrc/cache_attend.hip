@@ -502,6 +502,8 @@ struct RowsOf {
     }
 };
 
+#undef in_step
+
 __device__ __forceinline__ float lse_of(float m, float l) {
     return l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }

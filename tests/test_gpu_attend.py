@@ -314,3 +314,33 @@ def test_checked(monkeypatch):
         with pytest.raises(binding.TsError) as e:
             _run(bad)
         assert e.value.code == code, name
+
+
+def test_shared_pages():
+    # two sequences whose text begins alike read the same pages; their drafts lie in pages of their own
+    d = _inputs(2, 20, 4, 2, 64, 16, 200, "bfloat16", 11, True)
+    d["k"], d["v"] = d["k"].nan_to_num(0.2), d["v"].nan_to_num(0.2)
+    P, M = d["k"].shape[0], d["pages"].shape[1]
+    d["pages"] = np.random.default_rng(2).permutation(P)[:2 * M].reshape(2, M)
+    d["pages"][1, :9] = d["pages"][0, :9]
+    d["starts"], d["lengths"] = np.array([150, 144]), np.array([20, 17])
+    _compare(d, _run(d))
+
+
+def test_two_streams_at_once():
+    import torch
+    from paper_2002_00876_amd import binding
+    cases = [_inputs(12, N, 8, 2, 128, 16, 3000, "bfloat16", N, True) for N in (4, 40)]
+    want = [_run(d) for d in cases]
+    args = [(d["q"].cuda(), d["k"].cuda(), d["v"].cuda(), _ints(d["pages"]), _ints(d["starts"]),
+             _ints(d["parents"]), _ints(d["lengths"])) for d in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(5):
+        got = []
+        for s, a in zip(streams, args):
+            with torch.cuda.stream(s):
+                got.append(binding.tree_attention(*a))
+        torch.cuda.synchronize()
+        for g, x in zip(got, want):
+            assert torch.equal(g[0], x[0]) and torch.equal(g[1], x[1])
