@@ -5,9 +5,11 @@
 //   d L / d x_v = ([v = z] - p_v) / T,      d H / d x_v = - p_v (log p_v + H) / T.
 // In exponents to base 2, d = (x_v - m) log2(e) / T, p_v = 2^d / s and log p_v = d ln 2 - log s, so
 //   w dL + u dH = 2^d (gain + slope d) + [v = z] w / T,
-//   gain = -(w + u (H - log s)) / (T s),      slope = -u ln 2 / (T s):
+//   gain = -(w + u X) / (T s),      slope = -u ln 2 / (T s),      X = - ln 2 sum_v p_v d_v = H - log s:
 // one walk over the row gives its sums, a second one writes the gradient.  The sums leave z out, so that 1 - p
-// of a token that is nearly certain, and its log p, keep their digits: they are the others' sum.
+// of a token that is nearly certain, and its log p, keep their digits: they are the others' sum.  X is never
+// formed as the difference: log s is about 12 in a row of 131072 that is nearly uniform, and its rounding would
+// be an error that all tokens of the row share.
 //
 // Bound by reading and writing, and by what of the second read crosses the fabric: 8192 rows of 131072
 // bfloat16 with their gradient 815 us, 5.3 TB/s of one read and one write.
@@ -56,11 +58,10 @@ __device__ __forceinline__ Row finish(const ScoreArgs& a, uint32_t row, const T*
     others = spread_raise(others, m, c);
     const float s = others.s + e, t = others.t + d * e;
     const float ls = e == 1.f ? log1pf(others.s) : logf(fmaxf(s, 1.f));
-    const float entropy = ls - kLn2 * fminf(t, 0.f) / fmaxf(s, 1.f);
-    const float logp = z >= 0 ? (xz - m) * inv_t - ls : 0.f;
+    const float below = -kLn2 * fminf(t, 0.f) / fmaxf(s, 1.f);
     if (write) {
-        if (a.logp) a.logp[row] = logp;
-        if (a.entropy) a.entropy[row] = entropy;
+        if (a.logp) a.logp[row] = z >= 0 ? (xz - m) * inv_t - ls : 0.f;
+        if (a.entropy) a.entropy[row] = ls + below;
     }
     Row r{};
     if constexpr (kGrad) {
@@ -69,9 +70,9 @@ __device__ __forceinline__ Row finish(const ScoreArgs& a, uint32_t row, const T*
         if (!(s > 0.f)) w = u = 0.f;   // no finite logit
         const float f = s > 0.f ? 1.f / s : 0.f, p = e * f;
         r.m = m;
-        r.gain = -(w + u * (entropy - ls)) * f;
+        r.gain = -(w + u * below) * f;
         r.slope = -u * kLn2 * f;
-        r.at_z = w * (s > 0.f ? others.s * f : 1.f) - (p > 0.f ? u * p * (logp + entropy) : 0.f);
+        r.at_z = w * (s > 0.f ? others.s * f : 1.f) - (p > 0.f ? u * p * ((xz - m) * inv_t + below) : 0.f);
     }
     return r;
 }
