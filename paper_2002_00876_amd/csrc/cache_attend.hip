@@ -43,6 +43,22 @@ constexpr float kUp = std::is_same_v<T, F16> ? 14.f : 0.f;
 template <class T>
 constexpr float kLag = std::is_same_v<T, F16> ? 1.f : 8.f;
 
+// An exponent is s c2 - m, whose product is exact (an fma): it is rounded once, after the difference.  m is a
+// rounded product, so numerators of a row share a factor of up to 2^(half of m's last place), which the sums share
+// too.  Past kFarOut that could leave the types' range: the products are rounded as m is (what they lose is
+// what the scores themselves were rounded by), and the largest one's numerator is 2^kUp again.
+constexpr float kFarOut = 1 << 20;
+// What is taken from exponents of which `most` is the largest
+template <class T>
+__device__ __forceinline__ float base_of(float most) {
+    const float m = most - kUp<T>;
+    return most - m > kUp<T> + 0.5f ? most : m;   // floats that far out may lie further apart than kUp
+}
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+
 typedef float F4 __attribute__((ext_vector_type(4)));
 typedef uint32_t Quad __attribute__((ext_vector_type(4)));
 typedef short S4 __attribute__((ext_vector_type(4)));
@@ -442,18 +458,26 @@ struct RowsOf {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) most = fmaxf(most, s[x][t][e]);
             most = fmaxf(most, __shfl_xor(most, 16, kWave));
-            most = fmaxf(most, __shfl_xor(most, 32, kWave)) * c2 - kUp<T>;
-            if (__any(most > m[x] + kLag<T>)) {
+            most = base_of<T>(rounded_product(fmaxf(most, __shfl_xor(most, 32, kWave)), c2));
+            if (__any(most - m[x] > kLag<T>)) {
                 const float to = fmaxf(most, m[x]), f = exp2_(m[x] - to);
                 m[x] = to;
                 l[x] *= f;
 #pragma unroll
                 for (int t = 0; t < DP / 16; ++t) o[x][t] *= f;
             }
+            float c = c2;
+            if (__any(fabsf(m[x]) > kFarOut)) {
+                c = 1.f;
+#pragma unroll
+                for (int t = 0; t < KT / 16; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[x][t][e] = rounded_product(s[x][t][e], c2);
+            }
 #pragma unroll
             for (int t = 0; t < KT / 16; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[x][t][e] = fmaf(s[x][t][e], c2, -m[x]);
+                for (int e = 0; e < 4; ++e) s[x][t][e] = fmaf(s[x][t][e], c, -m[x]);
 #pragma unroll
             for (int t = 0; t < KT / 16; ++t)
 #pragma unroll
