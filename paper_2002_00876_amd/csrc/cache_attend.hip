@@ -32,7 +32,7 @@ constexpr int kSplitBatch = 256;      // most sequences whose slots are divided 
 constexpr int kWant = 512;            // workgroups that fill the chip
 constexpr int kWideRows = 2048;       // most rows whose parts are joined by a workgroup each
 constexpr float kLow = -1e30f;        // below every score
-constexpr float kNone = -1e36f;       // where a running maximum begins: below kLow * scale, the floats far
+constexpr float kNone = -1e37f;       // where a running maximum begins: below kLow times the largest c2, 1.44e6
 
 // A row's numerators are 2^(exponent - m + kUp), m its maximum so far: float16's smallest normal number
 // would otherwise be 2^-14 of the largest, and a long context's many small ones would lose their digits or

@@ -86,3 +86,33 @@ def test_large_scores_of_trees():
     parents = np.maximum(np.arange(N)[None] - rng.integers(1, 9, size=(len(sizes), N)), -1)
     _check(sizes, "bfloat16", N, 2, 1.0, parents, seed=2)
     _check(sizes[:6], "float16", N, 2, 1.0, parents[:6], seed=2)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16"])
+@pytest.mark.parametrize("N,G", SHAPES)
+@pytest.mark.parametrize("scale", [5e5, 1e6])
+def test_scores_at_the_lower_end(dtype, N, G, scale):
+    # every score of every row is -9.2e29 before the scale: the mean of the values that are seen, and a
+    # log-sum-exp whose rounding is that of its size
+    import torch
+    from paper_2002_00876_amd import binding
+    say(f"attend lower end N={N} G={G} scale={scale}")
+    D, S, past = 64, 16, 150
+    M = -(-(past + N) // S)
+    rng = np.random.default_rng(N)
+    q = torch.zeros((1, N, G, D), dtype=torch.bfloat16)
+    k = torch.zeros((M, S, 1, D), dtype=torch.bfloat16)
+    v = torch.from_numpy(rng.standard_normal((M, S, 1, D))).to(torch.bfloat16)
+    q[..., 0], k[..., 0] = -2.0 ** 50, 2.0 ** 49 * 1.453125
+    score = float(q[0, 0, 0, 0].double() * k[0, 0, 0, 0].double())
+    assert -1e30 < score < -9e29
+    out, lse = binding.tree_attention(q.cuda(), k.cuda(), v.cuda(), _ints([np.arange(M)]), _ints([past]), scale=scale)
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    flat = v.double().numpy().reshape(-1, D)
+    u = R.HALF_STEP["bfloat16"]
+    for i in range(N):
+        seen = flat[:past + i + 1]
+        want, mean = seen.mean(0), np.abs(seen).mean(0)
+        off = u * np.abs(want) + (u + 2.0 ** -21 + 2 * len(seen) * 2.0 ** -24) * mean + 2.0 ** -24
+        assert np.all(np.abs(out[0, i] - want) <= off), i
+    assert np.all(np.abs(lse - score * float(np.float32(scale))) <= 2.0 ** -22 * abs(score) * scale)
