@@ -186,7 +186,7 @@ ts_status ts_cache_attend(const void* q, const int64_t strides[3], int dtype, co
         if (N > kMaxNodes || !attend_fits(B, N, Hq, Hk, D, M * layout->page_size))
             return bad(call, TS_ERR_BAD_DIM, "N must be at most " + std::to_string(kMaxNodes) +
                                                  ", row tiles of all key heads 2^23, and a head's tiles of "
-                                                 "32 slots of them all 2^30 a workgroup");
+                                                 "32 slots of them all 2^31 a workgroup");
         if ((st = check_half(call, dtype)) || (st = check_aligned(call, "q", q, strides))) return st;
         if (!(scale >= 1e-6f && scale <= 1e6f))
             return bad(call, TS_ERR_BAD_ARG, "scale must be in [1e-6, 1e6]");

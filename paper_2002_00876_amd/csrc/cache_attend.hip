@@ -214,7 +214,7 @@ struct Walk {
         }
         total = uniform(total);
         const int most = (int)(gridDim.x / (unsigned)a.Hk);
-        per = uniform(max(p.least, (int)min((total + most - 1) / most, (uint64_t)1 << 30)));
+        per = uniform(max(p.least, (int)min((total + most - 1) / most, (uint64_t)INT32_MAX)));
         if (blockIdx.x == 0 && tid == 0) *p.per = per;
         // workgroups of an XCD take neighbouring stretches: row tiles of the same slots share its L2
         const int used = (int)((total + per - 1) / per) * a.Hk, many = (used + 7) / 8;
@@ -928,7 +928,8 @@ size_t attend_workspace(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D)
 bool attend_fits(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D, int64_t slots) {
     const AttendPlan p = attend_plan(B, N, Hq, Hk, D, nullptr);
     if (B * Hk * p.tiles > (int64_t)1 << 23) return false;   // 2^31 threads
-    return !p.split || B * p.tiles * (slots / 32 + 1) / (p.grid / Hk) < (int64_t)1 << 30;
+    // units of a stretch are an int; 2^35 slots are 2^30 tiles of 32, and each of up to 2^20 row tiles begins another
+    return !p.split || B * p.tiles * ((slots + 31) / 32) / (p.grid / Hk) < INT32_MAX;
 }
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {
     const AttendPlan p = attend_plan(a.B, a.N, a.Hq, a.Hk, a.D, a.ws);
