@@ -7,7 +7,8 @@
 //   w dL + u dH = 2^d (gain + slope d) + [v = z] w / T,
 //   gain = -(w + u X) / (T s),      slope = -u ln 2 / (T s),      X = - ln 2 sum_v p_v d_v = H - log s:
 // one walk over the row gives its sums, a second one writes the gradient.  The sums leave z out, so that 1 - p
-// of a token that is nearly certain, and its log p, keep their digits: they are the others' sum.  X is never
+// of a token that is nearly certain, and its log p, keep their digits: they are the others' sum; and one of
+// the others' largest logits, so that they do where another token is nearly certain.  X is never
 // formed as the difference: log s is about 12 in a row of 131072 that is nearly uniform, and its rounding would
 // be an error that all tokens of the row share.
 //
@@ -54,25 +55,31 @@ template <class T, bool kGrad>
 __device__ __forceinline__ Row finish(const ScoreArgs& a, uint32_t row, const T* x, int z, Spread others,
                                       bool write) {
     const float inv_t = a.scale.inv_t, c = a.scale.c, xz = z >= 0 ? to_f(x[z]) : -INFINITY;
+    const bool top = xz >= others.m;   // the given token is the one that the sums leave out
     const float m = fmaxf(others.m, xz), d = fmaxf((xz - m) * c, kNoTerm), e = exp2_(d);
-    others = spread_raise(others, m, c);
-    const float s = others.s + e, t = others.t + d * e;
-    const float ls = e == 1.f ? log1pf(others.s) : logf(fmaxf(s, 1.f));
-    const float below = -kLn2 * fminf(t, 0.f) / fmaxf(s, 1.f);
+    Spread all = others;
+    if (top) {
+        all = spread_raise(others, m, c);
+    } else {
+        all.s += all.whole() ? -e : e;
+        all.t += d * e;
+    }
+    const RowScore score(all);
     if (write) {
-        if (a.logp) a.logp[row] = z >= 0 ? (xz - m) * inv_t - ls : 0.f;
-        if (a.entropy) a.entropy[row] = ls + below;
+        if (a.logp) a.logp[row] = z >= 0 ? score.logp(xz, inv_t) : 0.f;
+        if (a.entropy) a.entropy[row] = score.entropy;
     }
     Row r{};
     if constexpr (kGrad) {
+        const float s = all.sum(), without = top ? all.s : others.sum();
         float w = z >= 0 ? (a.weights ? a.weights[row] : 1.f) * inv_t : 0.f;
         float u = a.entropy_weights ? a.entropy_weights[row] * inv_t : 0.f;
         if (!(s > 0.f)) w = u = 0.f;   // no finite logit
         const float f = s > 0.f ? 1.f / s : 0.f, p = e * f;
         r.m = m;
-        r.gain = -(w + u * below) * f;
+        r.gain = -(w + u * score.below) * f;
         r.slope = -u * kLn2 * f;
-        r.at_z = w * (s > 0.f ? others.s * f : 1.f) - (p > 0.f ? u * p * ((xz - m) * inv_t + below) : 0.f);
+        r.at_z = w * (s > 0.f ? without * f : 1.f) - (p > 0.f ? u * p * ((xz - m) * inv_t + score.below) : 0.f);
     }
     return r;
 }
@@ -153,7 +160,7 @@ __global__ __launch_bounds__(NT) void k_score(ScoreArgs a, int hold) {
             leave_out(v, i * W, z);
             const float t = max_of(v);
             most = fmaxf(most, t);
-            sums.raise(t, c);
+            sums.raise(v, t, c);
             sums.push(v, c);
         };
         int i = tid;
@@ -187,7 +194,7 @@ __global__ __launch_bounds__(NT) void k_score(ScoreArgs a, int hold) {
         if (e < V) {
             float one[1] = {e == z ? -INFINITY : to_f(x[e])};
             most = fmaxf(most, one[0]);
-            sums.raise(one[0], c);
+            sums.raise(one, one[0], c);
             sums.push(one, c);
         }
         Spread all = block_spread<NT>(sums.value(c), c, red);
@@ -259,7 +266,7 @@ __global__ __launch_bounds__(kPartThreads) void k_score_sums(ScoreArgs a, ScoreP
         leave_out(v, at, z);
         const float t = max_of(v);
         most = fmaxf(most, t);
-        sums.raise(t, c);
+        sums.raise(v, t, c);
         sums.push(v, c);
     });
     Spread s = block_spread<NT>(sums.value(c), c, red);
@@ -291,7 +298,7 @@ __global__ __launch_bounds__(kPartThreads) void k_score_parts(ScoreArgs a, Score
     const float c = a.scale.c;
     const int lane = threadIdx.x % kWave;
     const float4 s = lane < p.parts ? p.sums[(size_t)row * p.parts + lane]
-                                    : make_float4(-FLT_MAX, 0.f, 0.f, 0.f);
+                                    : make_float4(-FLT_MAX, -0.f, 0.f, 0.f);
     const int z = token_of(a, row);
     const Row r = finish<T, kGrad>(a, row, x, z, wave_spread({s.x, s.y, s.z}, c), first);
     if constexpr (kGrad)

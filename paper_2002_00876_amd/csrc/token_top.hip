@@ -197,15 +197,21 @@ __global__ __launch_bounds__(kWave) void k_top_short(TopArgs a) {
         }
         Spread sums = spread_empty();
         if constexpr (kScore) {
-            sums.m = wave_max_fast(soft.m);
+            const float m = wave_max_fast(soft.m);
+            bool one = false;
+#pragma unroll
+            for (int j = 0; j < J; ++j) one |= v[j] == m;
+            const bool any = __any(one);
+            if (first_lane(one)) leave_first_out(v, m);   // (v is not needed behind the sums)
+            float s = 0.f, t = 0.f;
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                const float d = fmaxf((v[j] - sums.m) * a.scale.c, kNoTerm), e = exp2_(d);
-                sums.s += e;
-                sums.t += d * e;
+                const float d = fmaxf((v[j] - m) * a.scale.c, kNoTerm), e = exp2_(d);
+                s += e;
+                t += d * e;
             }
-            sums.s = wave_sum_fast(sums.s);
-            sums.t = wave_sum_fast(sums.t);
+            s = wave_sum_fast(s);
+            sums = {m, any ? s : -s, wave_sum_fast(t)};
         } else {
 #pragma unroll
             for (int j = 0; j < J; ++j) soft.s += exp2_((v[j] - soft.m) * a.scale.c);
@@ -338,7 +344,7 @@ struct TopPlan {
     int parts;
     int64_t rows;     // of a slab
     float* least;     // [rows]
-    float4* sums;     // [rows][parts]: maximum and sum of the softmax, largest logit, entropy's sum
+    float4* sums;     // [rows][parts]: maximum and sum of the softmax (Spread's), largest logit, entropy's sum
     int32_t* count;   // [rows][parts][kScanWaves]: vectors that reach the threshold
     int32_t* at;      // [rows][parts][kScanWaves][kKeep]: their numbers
     Vec4* kept;       // [rows][parts][kScanWaves][kKeep]: and what they hold
@@ -460,8 +466,11 @@ __global__ __launch_bounds__(kScanThreads, 8) void k_top_scan(TopArgs a, TopPlan
     const int per = ((nv + p.parts - 1) / p.parts + 7) / 8 * 8;   // whole cache lines
     const int lo = min((int)part * per, nv), hi = min(lo + per, nv);
     const float c = a.scale.c, least = sh.least;
-    std::conditional_t<kScore, ChunkSpread, ChunkSoft> soft;
-    soft.init(a.scale);
+    std::conditional_t<kScore, WaveSpread<T>, ChunkSoft> soft;
+    if constexpr (kScore)
+        soft.init(a.scale, least);
+    else
+        soft.init(a.scale);
     float most = -INFINITY;
     int found = 0;   // of this wave
     auto keep = [&](bool reaches, const Raw<T>& r, int v) {
@@ -483,9 +492,16 @@ __global__ __launch_bounds__(kScanThreads, 8) void k_top_scan(TopArgs a, TopPlan
         }
         const float t = fmaxf(top[0], top[1]);
         most = fmaxf(most, t);
-        soft.raise(t, c);
+        if constexpr (kScore) {
+            const bool raised = soft.raise(r, t, c);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) soft.push(v[u], c);
+            for (int u = 0; u < 2; ++u) soft.push(v[u], c);
+            if (raised) soft.pushed(c);
+        } else {
+            soft.raise(t, c);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) soft.push(v[u], c);
+        }
         if (__any(t >= least)) {
             keep(top[0] >= least, r[0], v0);
             keep(top[1] >= least, r[1], v1);
@@ -509,19 +525,38 @@ __global__ __launch_bounds__(kScanThreads, 8) void k_top_scan(TopArgs a, TopPlan
         unpack<T>(r, one);
         const float t = i < hi ? max_of(one) : -INFINITY;
         most = fmaxf(most, t);
-        soft.raise(t, c);
-        if (i < hi) soft.push(one, c);
+        if constexpr (kScore) {
+            const Raw<T> q[1] = {r};
+            const bool raised = soft.raise(q, t, c);
+            if (i < hi) soft.push(one, c);
+            if (raised) soft.pushed(c);
+        } else {
+            soft.raise(t, c);
+            if (i < hi) soft.push(one, c);
+        }
         keep(t >= least, r, i);
     }
     const int e = nv * W + tid;   // the row's last few logits; k_top_pick looks at all of them
-    if (part == 0 && e < a.V) {
-        float one[1] = {to_f(x[e])};
+    if constexpr (kScore) {
+        if (part == 0 && nv * W < a.V) {
+            float one[W];
+#pragma unroll
+            for (int k = 0; k < W; ++k) one[k] = -INFINITY;
+            if (e < a.V) one[0] = to_f(x[e]);
+            most = fmaxf(most, one[0]);
+            const Raw<T> q[1] = {pack<T>(one)};
+            const bool raised = soft.raise(q, one[0], c);
+            soft.push(one, c);
+            if (raised) soft.pushed(c);
+        }
+    } else if (part == 0 && e < a.V) {
+        const float one[1] = {to_f(x[e])};
         most = fmaxf(most, one[0]);
         soft.raise(one[0], c);
         soft.push(one, c);
     }
     if constexpr (kScore) {
-        const Spread all = block_spread<NT>(soft.value(c), c, sh.red4);
+        const Spread all = join_spread<NT>(soft.value(c), c, sh.red4);
         most = block_max<NT>(most, (float*)sh.red);
         if (tid == 0) p.sums[blockIdx.x] = make_float4(all.m, all.s, most, all.t);
     } else {
@@ -588,7 +623,7 @@ __global__ __launch_bounds__(kTopThreads) void k_top_pick(TopArgs a, TopPlan p, 
     {
         const int lane = tid % kWave;
         const float4 s = lane < p.parts ? p.sums[(size_t)i * p.parts + lane]
-                                        : make_float4(-FLT_MAX, 0.f, -INFINITY, 0.f);
+                                        : make_float4(-FLT_MAX, kScore ? -0.f : 0.f, -INFINITY, 0.f);
         if constexpr (kScore)
             sums = wave_spread({s.x, s.y, s.w}, c);
         else
