@@ -353,24 +353,28 @@ __device__ __forceinline__ Place place_of(const AttendArgs& a, int head, int id,
 // 16 bytes a lane from `from` to LDS: those of the wave's lane l to `to` + 16 l, `to` the same in all.  once:
 // nothing else will read them, so they are not kept in the caches.  The load has no result that the compiler
 // would wait for, which its builtin makes it do at the next read of any LDS: loads_done() waits.  (M0 holds
-// the LDS address and is read one state after it is written; nothing else here uses it.)
+// the LDS address and is read one state after it is written.)
 __device__ __forceinline__ uint32_t lds_address(const void* at) {
     return (uint32_t)uniform((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)at);
 }
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // M0 is reserved: the compiler has to be told all the same
 __device__ __forceinline__ void load_to_lds(const short* from, short* to, bool once) {
     const uint32_t at = lds_address(to);
     if (once)
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"s"(at), "v"(from)
-                     : "memory");
+                     : "memory", "m0");
     else
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from)
-                     : "memory");
+                     : "memory", "m0");
 }
 // 4 bytes a lane, likewise
 __device__ __forceinline__ void load_id_to_lds(const int32_t* from, int32_t* to) {
     const uint32_t at = lds_address(to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(at), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(at), "v"(from)
+                 : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // Waits until at most `left` of the wave's loads are on their way (a barrier does not)
 template <int left>
