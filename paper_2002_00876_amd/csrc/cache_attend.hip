@@ -11,12 +11,16 @@
 // of 32, which is where the two score tiles left it.  V^T is read from LDS, where V lies as it does in
 // the cache, by the transposing read, four slots of one element a lane.
 //
-// Numerators are rounded to the cache's type for the product (their sum is not): each is off by half a
-// step at most, as the values are themselves, and the products are summed in 32 bits.
+// Products take 16-bit numerators.  Where a lane has one row (tiles of 64 rows), a numerator is two of them, a
+// cut one and its rest, whose product costs little beside the read: outputs are as good as with 32-bit numerators
+// (off by 2^-15 of a bfloat16's, 2^-21 of a float16's).  Where it has two, numerators are rounded to the cache's
+// type (their sum is not): each is off by half a step at most, as the values are themselves, which makes the error
+// of an output 1.4 times that of its own rounding.  Calls with both products and with one, us: 64 contexts of
+// up to 8000 slots (8 heads of 128, up to 5 drafts of 32 heads) 176 and 174; one of 131072 (4 heads of 64, 7 drafts
+// of 28) 38 and 37; 8 trees of 64 drafts of 64 heads over 4500 slots 135 and 113.
 //
-// Few rows are bound by the read: 64 contexts of up to 8000 slots, 8 heads of 128, with up to 5 drafts of 32
-// heads 162 us, 5.9 TB/s.  Many are bound by the products and the exponentials beside them, which two waves a
-// SIMD do not hide of each other: 8 trees of 64 drafts of 64 heads over 4500 slots 113 us, 645 TFLOP/s.
+// Few rows are bound by the read: the first of these calls has 0.96 GB, 5.5 TB/s.  Many are bound by the products
+// and the exponentials beside them, which two waves a SIMD do not hide of each other: the last one 640 TFLOP/s.
 #include <algorithm>
 
 #include "cache.h"
@@ -74,6 +78,29 @@ __device__ __forceinline__ F4 mma(S8 a, S8 b, F4 c) {
     else
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(H8, a),
                                                       __builtin_bit_cast(H8, b), c, 0, 0, 0);
+}
+
+// Two numerators, cut to T, and what was cut off, rounded to T
+typedef short S2 __attribute__((ext_vector_type(2)));
+struct Split {
+    S2 whole, rest;
+};
+template <class T>
+__device__ __forceinline__ Split split(float a, float b) {
+    float u, v;
+    S2 whole;
+    if constexpr (std::is_same_v<T, Bf16>) {
+        const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+        whole = __builtin_bit_cast(S2, __builtin_amdgcn_perm(y, x, 0x07060302u));
+        u = a - __uint_as_float(x & 0xffff0000u);
+        v = b - __uint_as_float(y & 0xffff0000u);
+    } else {
+        const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
+        whole = __builtin_bit_cast(S2, h);
+        u = a - (float)h[0];
+        v = b - (float)h[1];
+    }
+    return {whole, S2{(short)from_f<T>(u).u, (short)from_f<T>(v).u}};
 }
 
 // Four rows of 16 elements, 8 bytes a lane of each 16, turned: a lane gets its column's four
@@ -406,6 +433,7 @@ __device__ __forceinline__ S8 query(const AttendArgs& a, const Work& w, int r, i
 template <class T, int DP, int M, int KT>
 struct RowsOf {
     static constexpr int kPairs = KT / 32, kAhead = kAheadOf<M>;
+    static constexpr bool kRest = M == 1;   // numerators of two parts
     F4 o[M][DP / 16];
     float m[M], l[M];
 
@@ -453,7 +481,7 @@ struct RowsOf {
     }
 
     // Scores to numerators
-    __device__ __forceinline__ void numerators(F4 (&s)[M][KT / 16], S8 (&p)[M][kPairs], float c2) {
+    __device__ __forceinline__ void numerators(F4 (&s)[M][KT / 16], S8 (&p)[M][kPairs], S8 (&rest)[M][kPairs], float c2) {
 #pragma unroll
         for (int x = 0; x < M; ++x) {
             float most = kLow;
@@ -491,13 +519,24 @@ struct RowsOf {
             for (int t = 0; t < KT / 16; ++t) {
                 sum += (s[x][t][0] + s[x][t][1]) + (s[x][t][2] + s[x][t][3]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[x][t / 2][t % 2 * 4 + e] = (short)from_f<T>(s[x][t][e]).u;
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (!kRest) {
+                        p[x][t / 2][t % 2 * 4 + e] = (short)from_f<T>(s[x][t][e]).u;
+                    } else if (e % 2 == 0) {
+                        const Split two = split<T>(s[x][t][e], s[x][t][e + 1]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            p[x][t / 2][t % 2 * 4 + e + i] = two.whole[i];
+                            rest[x][t / 2][t % 2 * 4 + e + i] = two.rest[i];
+                        }
+                    }
+                }
             }
             l[x] += sum;
         }
     }
 
-    __device__ __forceinline__ void values(const short* V, const S8 (&p)[M][kPairs]) {
+    __device__ __forceinline__ void values(const short* V, const S8 (&p)[M][kPairs], const S8 (&rest)[M][kPairs]) {
         const int lane = threadIdx.x % kWave, row = lane % 16, quarter = lane / 16;
         const int slot = quarter * 4 + row / 4, swap = Tile<DP>::v_swap(slot);   // (the same for slot + 16)
         auto operand = [&](int i) {
@@ -514,9 +553,12 @@ struct RowsOf {
 #pragma unroll
         for (int i = 0; i < kAll; ++i) {
 #pragma unroll
-            for (int x = 0; x < M; ++x) o[x][i / kPairs] = mma<T>(f[i % kAhead], p[x][i % kPairs], o[x][i / kPairs]);
+            for (int x = 0; x < M; ++x) {
+                o[x][i / kPairs] = mma<T>(f[i % kAhead], p[x][i % kPairs], o[x][i / kPairs]);
+                if constexpr (kRest) o[x][i / kPairs] = mma<T>(f[i % kAhead], rest[x][i % kPairs], o[x][i / kPairs]);
+            }
             if (i + kAhead < kAll) f[i % kAhead] = operand(i + kAhead);
-            in_step(M, 2);
+            in_step((kRest ? 2 : 1) * M, 2);
         }
     }
 
@@ -691,7 +733,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
             }
             if (first >= w.s.rows) continue;
             F4 s[M][KT / 16];
-            S8 n[M][R::kPairs];
+            S8 n[M][R::kPairs], rest[M][R::kPairs];
             __builtin_amdgcn_s_setprio(1);   // (the other workgroup's wave then does its exponentials)
             rows.scores(sh.k[u % NS], q, s);
             __builtin_amdgcn_s_setprio(0);
@@ -704,9 +746,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_attend(AttendArgs a, AttendPlan
                         R::mask(s[x], y, seen(a, sh.words, i, u * KT + y * 32, w.start, w.end));
                 }
             }
-            rows.numerators(s, n, a.c2);
+            rows.numerators(s, n, rest, a.c2);
             __builtin_amdgcn_s_setprio(1);
-            rows.values(sh.v[u % NS], n);
+            rows.values(sh.v[u % NS], n, rest);
             __builtin_amdgcn_s_setprio(0);
         }
         rows.finish();
