@@ -23,9 +23,15 @@
 namespace tsc {
 namespace {
 
+// Few long rows are divided among workgroups, in two launches.  The second one costs 4 us of a call, which a row
+// walked by one workgroup takes at about 50000 bfloat16 tokens, and from some 500 rows on the chip is full without.
+// Divided and whole, us, the gradient: 16 rows of 32000 12.5 and 11.3, of 50001 12.6 and 15.3, of 131072 13.4 and
+// 28.3; 320 rows of 131072 46 and 50, 512 rows 71 and 59.
 constexpr int kPartThreads = 256;
-constexpr int kWantParts = 1024;   // workgroups that fill the chip
-constexpr int kMinPart = 4096;     // tokens of a part
+constexpr int kLongRow = 49152;    // tokens
+constexpr int kFewRows = 512;
+constexpr int kWantParts = 1024;   // workgroups that fill the chip (320 rows of 131072 with 512: 53 us)
+constexpr int kMinPart = 4096;     // tokens of a part (no difference from 2048 to 8192)
 // Vectors of a row that a thread holds in LDS between the two walks.  8192 rows of 131072 bfloat16 with
 // their gradient by 512 threads, us: 870 without, 850 with 2, 832 with 4, 815 with 6, 825 with 9 (two
 // workgroups a CU instead of three), 1026 with 10 (one); 859 by 1024 threads with 9.
@@ -230,7 +236,7 @@ struct ScorePlan {
 };
 ScorePlan score_plan(int64_t rows, int64_t V, void* ws) {
     ScorePlan p;
-    int64_t parts = (kWantParts + rows - 1) / rows;
+    int64_t parts = V > kLongRow && rows < kFewRows ? (kWantParts + rows - 1) / rows : 1;
     const int64_t most = (V + kMinPart - 1) / kMinPart;
     if (parts > most) parts = most;
     if (parts > kWave) parts = kWave;
@@ -351,12 +357,18 @@ hipError_t launch_score(const ScoreArgs& a, hipStream_t s) {
             else
                 k_score<T, NT, true, false><<<g, NT, lds, s>>>(a, hold);
         };
+        // Threads of a row, by what was measured (us, bfloat16, the gradient but where scores are named).  64 and
+        // 256: 16000 rows of 300 17.5 and 49, 4000 of 8192 28 and 33, 1000 of 4096 8.7 and 8.2, of 9000 17 and 13.
+        // 256 and 512: few rows, 16 of 20000 10.7 and 9.3, 512 of 50001 36 and 26; many, 2900 of 8192 27 and 34, of
+        // 32000 76 and 81, of 36000 95 and 87, of 131072 346 and 314; scores alone, which hold nothing of the row,
+        // 129 and 137.
+        const int64_t bytes = (int64_t)a.V * sizeof(T);
         if (a.V <= 1024 || (a.V <= 8192 && rows >= 2048))
             go(std::integral_constant<int, 64>{});
-        else if (a.V <= 24576)
-            go(std::integral_constant<int, 256>{});
-        else
+        else if (rows <= kFewRows ? bytes > 16384 : a.grad && bytes > 65536)
             go(std::integral_constant<int, 512>{});
+        else
+            go(std::integral_constant<int, 256>{});
     });
     return hipGetLastError();
 }
