@@ -13,7 +13,9 @@ namespace {
 
 constexpr int kAppendThreads = 256;
 constexpr int kAppendWaves = kAppendThreads / kWave;
-constexpr int64_t kWantTokens = 4096;   // waves that fill the chip
+// Up to so many tokens the waves of a workgroup share one's heads.  32 + 8 heads of 128, a wave a token and four,
+// us a call: 16 tokens 13.2 and 12.8, 512 13.1 and 12.9, 1024 13.1 and 13.2, 2048 16.1 and 18.2, 8192 39 and 55.
+constexpr int64_t kFewTokens = 1024;
 constexpr double kTurn = 0.15915494309189533577;   // 1 / (2 pi)
 
 typedef uint32_t Quad __attribute__((ext_vector_type(4)));   // 8 elements of 16 bits
@@ -37,7 +39,9 @@ __device__ __forceinline__ Quad pack8(const float (&v)[8]) {
 // What a token's vectors need: each lane has one chunk of a head (a pair of vectors to rotate, one of
 // neighbours, or one that is not rotated) and takes that of every so many heads.  `parts` waves share a
 // token's heads where tokens are few.  The first heads' vectors are asked for before the angles are formed
-// and the page is looked up: the three latencies pass together.
+// and the page is looked up: the three latencies pass together.  (112 VGPRs: three heads' pairs of vectors, the
+// 32-bit parts of a rotation, scalars kept in lanes.  No instruction touches the 20 bytes of scratch that the
+// compiler reports.)
 template <class T, bool kNeighbours>
 __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int parts) {
     constexpr int kU = 3;   // heads asked for at once
@@ -135,7 +139,7 @@ __global__ __launch_bounds__(kAppendThreads) void k_append(AppendArgs a, int par
 
 hipError_t launch_append(const AppendArgs& a, hipStream_t s) {
     const int64_t tokens = a.B * a.N;
-    const int parts = tokens < kWantTokens ? kAppendWaves : 1;
+    const int parts = tokens < kFewTokens ? kAppendWaves : 1;
     const unsigned grid = row_grid((tokens * parts + kAppendWaves - 1) / kAppendWaves, kAppendThreads);
     auto go = [&](auto t) {
         using T = decltype(t);

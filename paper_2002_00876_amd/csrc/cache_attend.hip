@@ -32,9 +32,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kWords = kMaxNodes / 32;
-constexpr int kSplitBatch = 256;      // most sequences whose slots are divided among workgroups
+// Most sequences whose slots are divided among workgroups, a thread each.  One more, of 1000 slots each, us a call:
+// 8 heads of 128 180 and 197, one 33 and 31; with one of 32000 slots among others of 200 88 and 690.
+constexpr int kSplitBatch = 256;
 constexpr int kWant = 512;            // workgroups that fill the chip
-constexpr int kWideRows = 2048;       // most rows whose parts are joined by a workgroup each
+// Most rows whose parts are joined by a workgroup each.  So and by tiles, us a call: 256 rows over 16000 slots 25
+// and 58, 2048 over 4 x 8000 43 and 50, 4096 over 8 x 4000 47.1 and 45.5, 8192 over 16 x 2000 52 and 43.
+constexpr int kWideRows = 2048;
 constexpr float kLow = -1e30f;        // below every score
 constexpr float kNone = -1e37f;       // where a running maximum begins: below kLow times the largest c2, 1.44e6
 
@@ -896,7 +900,10 @@ __global__ __launch_bounds__(kThreads) void k_attend_join_wide(AttendArgs a, Att
 
 // ---- launches ----
 
-// Row tiles of 64 or 128 rows.  (Heads of more than 128 elements leave no registers for a second row a lane.)
+// Row tiles of 64 or 128 rows.  (Heads of more than 128 elements leave no registers for a second row a lane.)  With
+// 64 and 128, rows of a key head and us a call: 64 contexts of 500 slots, 64 rows 38 and 42, 65 rows 65 and 44, 256
+// rows 132 and 90; 8 of 4000, 64 rows 46 and 50, 65 rows 46.4 and 47.7, 192 rows 81 and 59; one of 8000, 64 rows 26
+// and 27, 65 rows 30 and 27, 128 rows 30 and 35.
 int sixteens(int64_t N, int64_t Hq, int64_t Hk, int64_t D) { return N * (Hq / Hk) > 64 && D <= 128 ? 2 : 1; }
 
 AttendPlan attend_plan(int64_t B, int64_t N, int64_t Hq, int64_t Hk, int64_t D, void* ws) {
