@@ -13,7 +13,7 @@
 // be an error that all tokens of the row share.
 //
 // Bound by reading and writing, and by what of the second read crosses the fabric: 8192 rows of 131072
-// bfloat16 with their gradient 815 us, 5.3 TB/s of one read and one write.
+// bfloat16 with their gradient 819 us, 5.2 TB/s of one read and one write.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -33,8 +33,8 @@ constexpr int kFewRows = 512;
 constexpr int kWantParts = 1024;   // workgroups that fill the chip (320 rows of 131072 with 512: 53 us)
 constexpr int kMinPart = 4096;     // tokens of a part (no difference from 2048 to 8192)
 // Vectors of a row that a thread holds in LDS between the two walks.  8192 rows of 131072 bfloat16 with
-// their gradient by 512 threads, us: 870 without, 850 with 2, 832 with 4, 815 with 6, 825 with 9 (two
-// workgroups a CU instead of three), 1026 with 10 (one); 859 by 1024 threads with 9.
+// their gradient by 512 threads, us (with sums that took 4 less): 870 without, 850 with 2, 832 with 4, 815 with 6,
+// 825 with 9 (two workgroups a CU instead of three), 1026 with 10 (one); 859 by 1024 threads with 9.
 constexpr int kHold = 6;
 
 struct Row {

@@ -1,6 +1,7 @@
 // token_top.hip -- the K largest logits of every row, in order, and the row's log-sum-exp; or, with given
 // tokens (kScore), the K most likely tokens with their log-probabilities, the given one's, and the row's
-// entropy, whose sum is taken beside the softmax's (1.5 % of the scan's time).
+// entropy, whose sum is taken beside the softmax's (2 % of the scan's time for rows of 131072 tokens, 15 % for
+// rows of 32000).
 //
 // Logits are compared as 32-bit keys, a monotone image of the float (-0 counted as 0); a logit
 // and its index make one 64-bit word (key, ~index), so that the words of a row are all
