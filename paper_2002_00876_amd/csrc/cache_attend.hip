@@ -578,8 +578,11 @@ struct RowsOf {
 
 #undef in_step
 
+// (2^kUp is taken out of both before they are added: in the logarithm it would cost four bits)
+template <class T>
 __device__ __forceinline__ float lse_of(float m, float l) {
-    return l > 0.f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+    constexpr float one = 1.f / (1 << (int)kUp<T>);
+    return l > 0.f ? (m + kUp<T> + __builtin_amdgcn_logf(l * one)) * kLn2 : -INFINITY;
 }
 
 template <class T>
@@ -610,7 +613,7 @@ struct Target {
             if (at >= w.s.rows) l = 0.f;   // padding
             f = l > 0.f ? 1.f / l : 0.f;
             out = (T*)a.out + row * a.D;
-            if (first && a.lse) a.lse[row] = lse_of(m, l);
+            if (first && a.lse) a.lse[row] = lse_of<T>(m, l);
         }
     }
     __device__ __forceinline__ void store(int d, F4 o) const {
@@ -854,7 +857,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a, AttendPl
         add_parts(a, p, parts, r, d < a.D ? d : 0, 0, 1, pieces, m, &o, &l);
         const int64_t row = (b * a.N + in / G) * a.Hq + head * G + in % G;
         if (d < a.D) store4<T>((T*)a.out + row * a.D + d, o * (l > 0.f ? 1.f / l : 0.f));
-        if (d == 0 && a.lse) a.lse[row] = lse_of(m, l);
+        if (d == 0 && a.lse) a.lse[row] = lse_of<T>(m, l);
     }
 }
 
@@ -895,7 +898,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_join_wide(AttendArgs a, Att
 #pragma unroll
     for (int k = 0; k < kWaves; ++k) o += sums[k][lane], l += weights[k][lane];
     if (d < a.D) store4<T>((T*)a.out + (int64_t)row * a.D + d, o * (l > 0.f ? 1.f / l : 0.f));
-    if (d == 0 && a.lse) a.lse[row] = lse_of(m, l);
+    if (d == 0 && a.lse) a.lse[row] = lse_of<T>(m, l);
 }
 
 // ---- launches ----

@@ -55,3 +55,32 @@ def test_outputs_near_0(dtype, N, Hq, Hk, D, past):
     out, off = _bounds(d, dtype)
     far = np.abs(got - out) - off
     assert not np.isnan(got).any() and far.max() <= 0, (far.max(), np.unravel_index(far.argmax(), far.shape))
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("B,N,Hq,past", [(200, 8, 16, 3), (20, 33, 5, 0), (300, 8, 4, 3)])
+def test_log_sum_exp_near_0(B, N, Hq, past, dtype):
+    # few slots, whose scores are one exact product each.  An exponent to base 2 is rounded once (a float16's by
+    # 2^-21, for 2^14 is made of its row's largest), the factor to base 2 by 2^-24 of the score; the hardware
+    # exponential and logarithm are off by 2^-23 (of a sum of up to 2^3), sums by 2^-24 a slot, and the result,
+    # of m + log2 and its product with ln 2, by 2^-23 of itself and of m
+    D = 8
+    say(f"attend lse B={B} N={N} Hq={Hq} past={past} {dtype}")
+    d = _inputs(B, N, Hq, 1, D, 16, past, dtype, N, True)
+    d["q"][..., 1:], d["k"][..., 1:] = 0, d["k"][..., 1:] * 0     # (NaN stays where nothing is seen)
+    d["q"] *= 0.25
+    got = _run(d)[1].double().cpu().numpy()
+    q, k = (np.nan_to_num(d[x].double().numpy()) for x in "qk")
+    scale = float(np.float32(D ** -0.5))
+    for b in range(B):
+        n, start = int(d["lengths"][b]), int(d["starts"][b])
+        kk = R.slots(k, d["pages"], 16, b, start + n)[:, 0]
+        assert np.all(got[b, n:] == -np.inf)
+        for i in range(n):
+            to = R.sees(i, start, n, d["parents"][b])
+            for h in range(Hq):
+                s = scale * (kk[to] @ q[b, i, h])
+                want, size = np.log(np.exp(s).sum()), np.abs(s).max()
+                off = np.log(2) * (2.0 ** -21 if dtype == "float16" else 2.0 ** -23) + 2.0 ** -24 * size + 2.0 ** -23 + \
+                    max(1, np.log2(len(to))) * 2.0 ** -23 + len(to) * 2.0 ** -24 + 2.0 ** -23 * (abs(want) + size)
+                assert abs(got[b, i, h] - want) <= off, (b, i, h, got[b, i, h] - want, off)
