@@ -87,8 +87,9 @@ size_t ts_cache_attend_workspace_bytes(int64_t B, int64_t N, int64_t Hq, int64_t
  *            Where no slot is seen out is 0 and lse -inf, and so they are for padding.
  *   ws       device workspace of at least ts_cache_attend_workspace_bytes(...), aligned to 256
  *            bytes.  Its contents on entry are ignored.
- * Queries, keys and values of slots before starts[b] + lengths[b] are finite, and products q . k within
- * 1e30 in size; what lies behind these slots is never used.
+ * Queries, keys and values of slots before starts[b] + lengths[b] are finite, products q . k within 1e30
+ * in size and values within 1e27 (sums of up to 2^30 of them, with numerators of up to 2^8, stay 32-bit
+ * floats); what lies behind these slots is never used.
  */
 ts_status ts_cache_attend(const void* q, const int64_t strides[3], int dtype, const void* k_cache,
                           const void* v_cache, const ts_cache_layout* layout,

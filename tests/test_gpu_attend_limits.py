@@ -116,3 +116,18 @@ def test_scores_at_the_lower_end(dtype, N, G, scale):
         off = u * np.abs(want) + (u + 2.0 ** -21 + 2 * len(seen) * 2.0 ** -24) * mean + 2.0 ** -24
         assert np.all(np.abs(out[0, i] - want) <= off), i
     assert np.all(np.abs(lse - score * float(np.float32(scale))) <= 2.0 ** -22 * abs(score) * scale)
+
+
+@pytest.mark.parametrize("N,G", SHAPES)
+def test_values_of_any_size(N, G):
+    # values times a power of two: outputs are the same bits times it, up to the stated size
+    import torch
+    from test_gpu_attend import _inputs, _run
+    d = _inputs(2, N, G, 1, 64, 16, 300, "bfloat16", N, True)
+    d["q"] = d["q"] * 4
+    want, lse = _run(d)
+    for e in (-60, 60, 86):
+        large = dict(d, v=d["v"] * 2.0 ** e)
+        got, other = _run(large)
+        assert float(large["v"].nan_to_num(0).abs().max()) <= 1e27
+        assert torch.equal(got.double(), want.double() * 2.0 ** e) and torch.equal(lse, other), e
