@@ -376,50 +376,12 @@ __device__ __forceinline__ void push_chunk(const float (&v)[W], float c, float r
     s += e[0];
 }
 
-// ChunkSoft's sums with the entropy's, without one of the logits m where `one` says so
-struct ChunkSpread {
-    float m, r, s, t;
-    bool one;
-    __device__ __forceinline__ void init(const Scale& k) {
-#pragma clang fp contract(off)
-        m = -k.most, r = m * k.c, s = t = 0.f, one = false;
-    }
-    __device__ __forceinline__ void to(float most, float c) {
-#pragma clang fp contract(off)
-        const float r2 = most * c, d = fmaxf(r - r2, kNoTerm), f = exp2_(d);
-        const float d1 = one ? fmaxf(fmaf(m, c, -r2), kNoTerm) : kNoTerm, e1 = exp2_(d1);
-        t = (t + s * d) * f + d1 * e1;
-        s = s * f + e1;
-        m = most;
-        r = r2;
-    }
-    // Before v is pushed, whose largest is `most`; v loses the one that is left out from then on
-    template <int W>
-    __device__ __forceinline__ void raise(float (&v)[W], float most, float c) {
-        if (most > m) {
-            to(most, c);
-            one = true;
-            leave_first_out(v, most);
-        }
-    }
-    template <int W>
-    __device__ __forceinline__ void push(const float (&v)[W], float c) {
-        push_chunk(v, c, r, s, t);
-    }
-    __device__ __forceinline__ Spread value(float c) const {
-#pragma clang fp contract(off)
-        if (!one && !(s > 0.f)) return spread_empty();
-        const float d = -fmaf(m, c, -r), f = exp2_(d);   // what r was rounded by
-        return {m, one ? s * f : -(s * f), (t + s * d) * f};
-    }
-};
-
-// The same for vectors of T of a whole wave, whose lanes have one maximum and call all this together: it is
-// hardly ever raised.  The vectors with the maximum are not pushed by the lane that has them but wait as
-// `words`, a word a lane, to be summed when they have it no longer, or without one m in the end.  (The scan of
-// top logits with it, 4096 rows of 131072 and 3000 of 32000 bfloat16: 185 and 45.9 us; with ChunkSpread, whose
-// lanes each take a logit out of 16 at every raise of their own: 191 and 48.2; with sums that leave none out and
-// have no digits beside 1: 185 and 44.4.)
+// ChunkSoft's sums with the entropy's, of vectors of T of a whole wave, whose lanes have one maximum and call all
+// this together: it is hardly ever raised.  The vectors with the maximum are not pushed by the lane that has them
+// but wait as `words`, a word a lane, to be summed when they have it no longer, or without one m in the end.  (The
+// scan of top logits with it, 4096 rows of 131072 and 3000 of 32000 bfloat16: 185 and 45.9 us; with lanes that
+// each take a logit out of 16 at every raise of their own 191 and 48.2; with sums that leave none out and have no
+// digits beside 1 185 and 44.4.)
 template <class T>
 struct WaveSpread {
     float m, r, s, t;
@@ -441,9 +403,10 @@ struct WaveSpread {
             else
                 v[k] = to_f(T{(uint16_t)(words >> 16 * k)});
     }
-    // Before the vectors q are pushed, whose largest logit is `most`; where it says so, pushed() follows
+    // Before the vectors q are pushed, whose largest logit is `most` (but for the one at `skip`, which is not
+    // pushed either); where it says so, pushed() follows
     template <int U>
-    __device__ __forceinline__ bool raise(const Raw<T> (&q)[U], float most, float c) {
+    __device__ __forceinline__ bool raise(const Raw<T> (&q)[U], float most, float c, int skip = -1) {
 #pragma clang fp contract(off)
         if (!__any(most > m)) return false;
         const float top = wave_max_fast(most), r2 = top * c, d = fmaxf(r - r2, kNoTerm), f = exp2_(d);
@@ -462,6 +425,12 @@ struct WaveSpread {
                 words = lane == u * 4 + k ? x : words;
             }
         if (U == 1 && lane >= 4) words = kNothing;
+        skip = __builtin_amdgcn_readlane(skip, who);
+        if (kEach == 1) {
+            if (lane == skip) words = kNothing;
+        } else if (skip >= 0 && lane == skip / 2) {
+            words = skip & 1 ? (words & 0xffffu) | (kNothing & 0xffff0000u) : (words & 0xffff0000u) | (kNothing & 0xffffu);
+        }
         if (lane == who) r = INFINITY;   // nothing of its vectors then has a numerator
         return true;
     }
@@ -492,13 +461,21 @@ struct WaveSpread {
     }
 };
 
+// log(1 + x), x >= 0.  Up to 1/2: 2 atanh(x / (2 + x)) by its series, whose first term left out is below 2^-26 of it
+// (log1pf, for any x, takes a row of 300 tokens 14 % of its time).
+__device__ __forceinline__ float log1p_(float x) {
+    if (x > 0.5f) return logf(1.f + x);
+    const float s = x * __builtin_amdgcn_rcpf(2.f + x), q = s * s;
+    return 2.f * s * fmaf(q, fmaf(q, fmaf(q, fmaf(q, 1.f / 9, 1.f / 7), 1.f / 5), 1.f / 3), 1.f);
+}
+
 // What a row's scores are made of, from the sums of its softmax: log p_v = (x_v - m) / T - ls, and the
 // entropy.  (A rest below 0 is rounding, or that of a row without a finite logit, which has no p: its log p are
 // -inf, its entropy 0.)
 struct RowScore {
     float m, ls, below, entropy;   // below: the entropy less log s
     __device__ __forceinline__ explicit RowScore(Spread a)
-        : m(a.m), ls(log1pf(fmaxf(a.rest(), 0.f))), below(-kLn2 * fminf(a.t, 0.f) / fmaxf(a.sum(), 1.f)),
+        : m(a.m), ls(log1p_(fmaxf(a.rest(), 0.f))), below(-kLn2 * fminf(a.t, 0.f) / fmaxf(a.sum(), 1.f)),
           entropy(ls + below) {}
     __device__ __forceinline__ float logp(float x, float inv_t) const { return (x - m) * inv_t - ls; }
 };

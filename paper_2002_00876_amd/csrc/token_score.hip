@@ -122,6 +122,39 @@ __device__ __forceinline__ void write_zeros(T* grad, int lo, int hi) {
     if (e < hi) grad[e] = from_f<T>(0.f);
 }
 
+// A wave's sums without z: its lanes call all this together, for vectors that begin at token `at`
+template <class T>
+struct RowSums {
+    static constexpr int W = kVec<T>;
+    WaveSpread<T> sums;
+    float most, c;   // the largest logit
+    int z;
+    __device__ __forceinline__ void init(const Scale& k, int z_) {
+        sums.init(k, -INFINITY);
+        most = -INFINITY, c = k.c, z = z_;
+    }
+    // there: otherwise the lane has no vector
+    __device__ __forceinline__ void push(const Raw<T>& r, int at, bool there) {
+        float v[W];
+        unpack<T>(r, v);
+        leave_out(v, at, z);
+        const float t = there ? max_of(v) : -INFINITY;
+        most = fmaxf(most, t);
+        const Raw<T> q[1] = {r};
+        const bool raised = sums.raise(q, t, c, (unsigned)(z - at) < (unsigned)W ? z - at : -1);
+        if (there) sums.push(v, c);
+        if (raised) sums.pushed(c);
+    }
+    // Token e alone, where it is below `end`
+    __device__ __forceinline__ Raw<T> one(const T* x, int e, int end) const {
+        float v[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) v[k] = -INFINITY;
+        if (e < end) v[0] = to_f(x[e]);
+        return pack<T>(v);
+    }
+};
+
 // Sums of tokens [lo, hi) the slow way that any logits allow
 template <class T, int NT>
 __device__ Spread sums_again(const T* x, int lo, int hi, int z, float c, float4* red) {
@@ -157,54 +190,39 @@ __global__ __launch_bounds__(NT) void k_score(ScoreArgs a, int hold) {
         auto from = [&](int i) { return (const T*)((const char*)x + (uint32_t)i * 16u); };
         auto to = [&](int i) { return (T*)((char*)grad + (uint32_t)i * 16u); };
         const int z = token_of(a, row);
-        ChunkSpread sums;
-        sums.init(a.scale);
-        float most = -INFINITY;
-        auto push = [&](const Raw<T>& r, int i) {
-            float v[W];
-            unpack<T>(r, v);
-            leave_out(v, i * W, z);
-            const float t = max_of(v);
-            most = fmaxf(most, t);
-            sums.raise(v, t, c);
-            sums.push(v, c);
-        };
+        RowSums<T> sums;
+        sums.init(a.scale, z);
         int i = tid;
         const int kept = kGrad ? min(hold * NT, nv) : 0;   // vectors that are
         if constexpr (kGrad) {
-            for (; i + (kU - 1) * NT < kept; i += kU * NT) {
+            for (; (i | (kWave - 1)) + (kU - 1) * NT < kept; i += kU * NT) {
                 Raw<T> r[kU];
 #pragma unroll
                 for (int u = 0; u < kU; ++u) r[u] = load_raw<T, true>(from(i + u * NT));
 #pragma unroll
                 for (int u = 0; u < kU; ++u) {
                     held[i + u * NT] = make_uint4(r[u].w[0], r[u].w[1], r[u].w[2], r[u].w[3]);
-                    push(r[u], i + u * NT);
+                    sums.push(r[u], (i + u * NT) * W, true);
                 }
             }
-            for (; i < kept; i += NT) {
-                const Raw<T> r = load_raw<T, true>(from(i));
-                held[i] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
-                push(r, i);
+            for (; (i & ~(kWave - 1)) < kept; i += NT) {
+                const Raw<T> r = load_raw<T, true>(from(min(i, kept - 1)));
+                if (i < kept) held[i] = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+                sums.push(r, i * W, i < kept);
             }
         }
-        for (; i + (kU - 1) * NT < nv; i += kU * NT) {
+        for (; (i | (kWave - 1)) + (kU - 1) * NT < nv; i += kU * NT) {
             Raw<T> r[kU];
 #pragma unroll
             for (int u = 0; u < kU; ++u) r[u] = load_raw<T, !kGrad>(from(i + u * NT));
 #pragma unroll
-            for (int u = 0; u < kU; ++u) push(r[u], i + u * NT);
+            for (int u = 0; u < kU; ++u) sums.push(r[u], (i + u * NT) * W, true);
         }
-        for (; i < nv; i += NT) push(load_raw<T, !kGrad>(from(i)), i);
+        for (; (i & ~(kWave - 1)) < nv; i += NT) sums.push(load_raw<T, !kGrad>(from(min(i, nv - 1))), i * W, i < nv);
         const int e = nv * W + tid;   // the row's last few tokens
-        if (e < V) {
-            float one[1] = {e == z ? -INFINITY : to_f(x[e])};
-            most = fmaxf(most, one[0]);
-            sums.raise(one, one[0], c);
-            sums.push(one, c);
-        }
-        Spread all = block_spread<NT>(sums.value(c), c, red);
-        if (far(block_max<NT>(most, (float*)red), a.scale)) all = sums_again<T, NT>(x, 0, V, z, c, red);
+        if (nv * W < V) sums.push(sums.one(x, e, V), e, true);
+        Spread all = join_spread<NT>(sums.sums.value(c), c, red);
+        if (far(block_max<NT>(sums.most, (float*)red), a.scale)) all = sums_again<T, NT>(x, 0, V, z, c, red);
         const Row r = finish<T, kGrad>(a, row, x, z, all, tid == 0);
         if constexpr (kGrad) {
             if (e < V) grad[e] = from_f<T>(e == z ? r.at_z : grad_of<kEntropy>(to_f(x[e]), r, c));
@@ -265,18 +283,24 @@ __global__ __launch_bounds__(kPartThreads) void k_score_sums(ScoreArgs a, ScoreP
     int lo, hi;
     part_range(a.V, p.parts, part, &lo, &hi);
     const int z = token_of(a, row);
-    ChunkSpread sums;
-    sums.init(a.scale);
-    float most = -INFINITY;
-    walk_row<T, NT, 4>(x, lo, hi, threadIdx.x, [&](float (&v)[W], int at, int) {
-        leave_out(v, at, z);
-        const float t = max_of(v);
-        most = fmaxf(most, t);
-        sums.raise(v, t, c);
-        sums.push(v, c);
-    });
-    Spread s = block_spread<NT>(sums.value(c), c, red);
-    most = block_max<NT>(most, (float*)red);
+    RowSums<T> sums;
+    sums.init(a.scale, z);
+    constexpr int kU = 4;
+    const int nv = (hi - lo) / W;
+    int i = threadIdx.x;
+    for (; (i | (kWave - 1)) + (kU - 1) * NT < nv; i += kU * NT) {
+        Raw<T> r[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) r[u] = load_raw<T, false>(x + lo + (size_t)(i + u * NT) * W);
+#pragma unroll
+        for (int u = 0; u < kU; ++u) sums.push(r[u], lo + (i + u * NT) * W, true);
+    }
+    for (; (i & ~(kWave - 1)) < nv; i += NT)
+        sums.push(load_raw<T, false>(x + lo + (size_t)min(i, nv - 1) * W), lo + i * W, i < nv);
+    const int e = lo + nv * W + (int)threadIdx.x;
+    if (lo + nv * W < hi) sums.push(sums.one(x, e, hi), e, true);
+    Spread s = join_spread<NT>(sums.sums.value(c), c, red);
+    const float most = block_max<NT>(sums.most, (float*)red);
     if (most != -INFINITY && far(most, a.scale)) s = sums_again<T, NT>(x, lo, hi, z, c, red);
     if (threadIdx.x == 0) p.sums[blockIdx.x] = make_float4(s.m, s.s, s.t, 0.f);
 }
