@@ -84,13 +84,14 @@ __device__ __forceinline__ F4 mma(S8 a, S8 b, F4 c) {
                                                       __builtin_bit_cast(H8, b), c, 0, 0, 0);
 }
 
-// Two numerators, cut to T, and what was cut off, rounded to T
+// Two numerators, cut to T, and what was cut off, rounded to T.  minus is -1, which the compiler does not know: a
+// conversion from float16, a product and a sum are one instruction, a conversion and a difference two.
 typedef short S2 __attribute__((ext_vector_type(2)));
 struct Split {
     S2 whole, rest;
 };
 template <class T>
-__device__ __forceinline__ Split split(float a, float b) {
+__device__ __forceinline__ Split split(float a, float b, float minus) {
     float u, v;
     S2 whole;
     if constexpr (std::is_same_v<T, Bf16>) {
@@ -101,8 +102,8 @@ __device__ __forceinline__ Split split(float a, float b) {
     } else {
         const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
         whole = __builtin_bit_cast(S2, h);
-        u = a - (float)h[0];
-        v = b - (float)h[1];
+        u = fmaf((float)h[0], minus, a);
+        v = fmaf((float)h[1], minus, b);
     }
     return {whole, S2{(short)from_f<T>(u).u, (short)from_f<T>(v).u}};
 }
@@ -518,7 +519,8 @@ struct RowsOf {
             for (int t = 0; t < KT / 16; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[x][t][e] = exp2_(s[x][t][e]);
-            float sum = 0.f;
+            float sum = 0.f, minus = -1.f;
+            asm("" : "+s"(minus));
 #pragma unroll
             for (int t = 0; t < KT / 16; ++t) {
                 sum += (s[x][t][0] + s[x][t][1]) + (s[x][t][2] + s[x][t][3]);
@@ -527,7 +529,7 @@ struct RowsOf {
                     if constexpr (!kRest) {
                         p[x][t / 2][t % 2 * 4 + e] = (short)from_f<T>(s[x][t][e]).u;
                     } else if (e % 2 == 0) {
-                        const Split two = split<T>(s[x][t][e], s[x][t][e + 1]);
+                        const Split two = split<T>(s[x][t][e], s[x][t][e + 1], minus);
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             p[x][t / 2][t % 2 * 4 + e + i] = two.whole[i];
